@@ -17,7 +17,7 @@ An 8-bit pool holds e4m3 numbers and one power-of-two scale 2^(s-127), s a byte,
 s is the smallest with which the largest finite |x| of the block's rows is at most 448.  Rows join a partly filled block at
 the larger of its scale and theirs, and what it held is rounded anew to a larger one.  Numbers that are not finite become NaN.
 One block of a plane: [kv_heads] tiles of 16 * head_dim bytes, [kv_heads] scale bytes, padding to 16.  A K tile is
-[head_dim / 16][token][16], a V tile [token / 4][16][head_dim / 16][token % 4] with element 16 * third + second.
+[head_dim / 16][token][16], a V tile [head_dim / 64][token / 4][16][4][token % 4] with element 64 * first + 16 * fourth + third.
 
 K and V are of unit variance with queries of standard deviation 2 (a moderately sharp softmax); blocks sit at random places of
 the pool, as after hours of evictions.
@@ -185,7 +185,8 @@ def _pack(x, is_k):
     d = x.shape[-1]
     if is_k:
         return x.unflatten(-1, (d // 16, 16)).transpose(-3, -2).flatten(-3)
-    return x.unflatten(-1, (d // 16, 16)).unflatten(-3, (4, 4)).movedim(-3, -1).transpose(-3, -2).flatten(-4)
+    x = x.unflatten(-1, (d // 64, 4, 16)).unflatten(-4, (4, 4))  # [..., token / 4, token % 4, d / 64, d % 64 / 16, d % 16]
+    return x.movedim((-3, -5, -1, -2, -4), (-5, -4, -3, -2, -1)).flatten(-5)
 
 
 def _unpack(tile, is_k):
@@ -193,7 +194,8 @@ def _unpack(tile, is_k):
     d = tile.shape[-1] // BLOCK
     if is_k:
         return tile.unflatten(-1, (d // 16, 16, 16)).transpose(-3, -2).flatten(-2)
-    return tile.unflatten(-1, (4, 16, d // 16, 4)).transpose(-3, -2).movedim(-1, -3).flatten(-2).flatten(-3, -2)
+    x = tile.unflatten(-1, (d // 64, 4, 16, 4, 4))
+    return x.movedim((-5, -4, -3, -2, -1), (-3, -5, -1, -2, -4)).flatten(-3).flatten(-3, -2)
 
 
 def prepare(case, seed):
@@ -420,7 +422,7 @@ def _exact_round(x):
 def _exact_order(d, is_k):
     """Byte of a tile for each (token, element)."""
     t, e = np.meshgrid(np.arange(BLOCK), np.arange(d), indexing="ij")
-    at = (e // 16 * 16 + t) * 16 + e % 16 if is_k else ((t // 4 * 16 + e % 16) * (d // 16) + e // 16) * 4 + t % 4
+    at = (e // 16 * 16 + t) * 16 + e % 16 if is_k else (((e // 64 * 4 + t // 4) * 16 + e % 16) * 4 + e % 64 // 16) * 4 + t % 4
     return torch.from_numpy(at).cuda()
 
 
