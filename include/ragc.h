@@ -26,7 +26,8 @@
  *     the new tokens are then partly written.  ragc_last_error() gives a thread-local
  *     message.
  *   - Block size is 16 tokens.  head_dim is 64 or 128.  dtype is fp32 or bf16 and is
- *     the type of the pool, of q/k_new/v_new and of the output.
+ *     the type of the pool, of q/k_new/v_new and of the output; 8-bit pools have calls of
+ *     their own (ragc_kv8_append, ragc_kv8_attn).
  *
  * Pool layout.  Two planes, K and V, each
  *       [num_blocks][kv_heads][16][head_dim]           (row-major)
@@ -105,9 +106,21 @@ typedef enum ragc_status {
     RAGC_ERR_WORKSPACE = -6  /* workspace missing or too small */
 } ragc_status;
 
-typedef enum ragc_dtype { RAGC_DTYPE_F32 = 0, RAGC_DTYPE_BF16 = 1 } ragc_dtype;
+typedef enum ragc_dtype {
+    RAGC_DTYPE_F32 = 0,
+    RAGC_DTYPE_BF16 = 1,
+    RAGC_DTYPE_E4M3 = 2 /* 8-bit pools only: ragc_kv8_append, ragc_kv8_attn, ragc_kv_swap */
+} ragc_dtype;
 
-/* Paged K/V pool of one layer. */
+/* Paged K/V pool of one layer.
+ *
+ * 8-bit pools (RAGC_DTYPE_E4M3).  Numbers are e4m3 (OCP: 448 the largest, 0x7f and 0xff NaN) times a power of two
+ * 2^(s-127), one byte s of 1..254 for each block, plane and kv head.  One block of a plane is
+ *       [kv_heads] tiles of 16*head_dim bytes, [kv_heads] scale bytes, padding to a multiple of 16
+ *   and block_stride_elems counts bytes.  Element d of token t of a tile is byte
+ *       K  (d/16 * 16 + t) * 16 + d%16                            [head_dim/16][token][16]
+ *       V  (((d/64 * 4 + t/4) * 16 + d%16) * 4 + d%64/16) * 4 + t%4    [head_dim/64][token/4][16][4][token%4]
+ *   the order in which the matrix cores take their operands.  q, k_new, v_new and out are bf16. */
 typedef struct ragc_kv_pool {
     void* k;                    /* [device] K plane */
     void* v;                    /* [device] V plane */
@@ -119,6 +132,17 @@ typedef struct ragc_kv_pool {
     int32_t reserved;           /* must be 0 */
     int64_t block_stride_elems; /* elements between blocks of one plane */
 } ragc_kv_pool;
+
+/* Rotation of Q and K by their positions.  Row p of cos_sin holds the cos of the rot_dim/2 angles of position p, then
+ * their sin, in fp32, with whatever scaling of angles or lengths the model has worked in.  Pair i of a head becomes
+ * (a cos_i - b sin_i, a sin_i + b cos_i); elements from rot_dim on stay. */
+typedef struct ragc_rope {
+    const float* cos_sin;  /* [device] [positions][rot_dim] */
+    int32_t positions;     /* rows of cos_sin; every new token's position lies below */
+    int32_t rot_dim;       /* a multiple of 16, 16 to head_dim */
+    int32_t interleaved;   /* pairs are elements 0: i and i + rot_dim/2, 1: 2i and 2i + 1 */
+    int32_t reserved;      /* must be 0 */
+} ragc_rope;
 
 /* One batch of augmented requests.  The request's document sequence has already
  * been matched against the tree by the caller: what arrives here is the block
@@ -276,6 +300,26 @@ int ragc_prefill_attn_static(const ragc_kv_pool* pool, const ragc_batch* batch, 
 int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new,
                    void* stream);
 
+/* ragc_kv_append with the position rotation on the way: K of the new tokens is turned by the angles of positions
+ * prefix_len[r]+i and stored, V is stored as it is, and Q is turned too, in one launch.  Computed in fp32, rounded once.
+ *   q, q_out    [device] [sum new_len][q_heads][head_dim]; both NULL with q_heads 0 where Q is not to be turned
+ *   k_out       [device] the turned K packed like k_new, what ragc_prefill_attn takes for k_new (without
+ *               RAGC_ATTN_APPEND_FUSED: the pool has the rows already); NULL where only the pool is wanted
+ * q_out may be q and k_out k_new (turned in place); otherwise an output overlaps no input.
+ * All device arrays are read when the work runs; a captured call replays with the sum of new_len of the capture. */
+int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q,
+                        const void* k_new, const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream);
+
+/* ragc_kv_append_rope into an 8-bit pool; rows are bf16, rope may be NULL (nothing turns; then no Q either).
+ * A block's scale byte is s = e + 127 with e the smallest integer for which the largest finite |x| of the tokens that join
+ * it is at most 448 * 2^e (1 where that is 0 or less than 448 * 2^-126), and x is stored as the e4m3 number
+ * nearest to x * 2^-e, ties to even, of the exact turned x; what is not finite becomes NaN (0x7f).  Tokens that join a block
+ * which holds some already (slot 0 is not among the new ones) take the larger of its scale and theirs, and where
+ * that is theirs the ones it holds are rounded anew (exact for all that stay normal numbers).  The slots behind
+ * the last token keep their bytes; bytes of V next to those that change are written back as they were. */
+int ragc_kv8_append(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
+                    const void* v_new, void* q_out, int32_t q_heads, void* stream);
+
 /* Copy whole blocks (all kv heads, K and V planes) between the device pool and a
  * pinned host pool of the same per-block layout (Sec. 5.1 "Swap out only once";
  * Sec. 3.2 "Cache hit": the transfer is part of the hit latency).
@@ -284,6 +328,7 @@ int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void
  *   dev_block_ids, host_slots [host] n entries each; pair i moves device block
  *                             dev_block_ids[i] <-> host slot host_slots[i]
  *   direction                 RAGC_SWAP_TO_DEVICE or RAGC_SWAP_TO_HOST
+ * 8-bit pools: blocks move with their scales, [kv_heads] tiles, scale bytes and padding, the stride in bytes.
  * The id arrays are read before the call returns.  `stream` is normally a side
  * stream; the caller orders it against attention with events.  A byte copy. */
 int ragc_kv_swap(const ragc_kv_pool* pool, void* host_k, void* host_v, int64_t host_block_stride_elems,

@@ -20,13 +20,14 @@ LIB_PATH = os.path.join(_HERE, "libragc.so")
 
 RAGC_OK = 0
 RAGC_ERR_NULL, RAGC_ERR_SHAPE, RAGC_ERR_RANGE, RAGC_ERR_ALIGN, RAGC_ERR_HIP, RAGC_ERR_WORKSPACE = -1, -2, -3, -4, -5, -6
-RAGC_DTYPE_F32, RAGC_DTYPE_BF16 = 0, 1
+RAGC_DTYPE_F32, RAGC_DTYPE_BF16, RAGC_DTYPE_E4M3 = 0, 1, 2
 RAGC_ATTN_APPEND_FUSED, RAGC_ATTN_NO_SPLIT, RAGC_ATTN_VALIDATE = 0x1, 0x2, 0x4
 RAGC_SWAP_AUTO, RAGC_SWAP_MEMCPY, RAGC_SWAP_KERNEL = 0, 1, 2
 RAGC_SWAP_TO_DEVICE, RAGC_SWAP_TO_HOST = 0, 1
 
 EXPORTS = ["ragc_version", "ragc_last_error", "ragc_kv_bytes_per_token", "ragc_prefill_attn_workspace",
            "ragc_prefill_attn", "ragc_prefill_attn_static", "ragc_kv_append", "ragc_kv_swap", "ragc_kv_gather",
+           "ragc_kv_append_rope", "ragc_kv8_append",
            "ragc_batch_validate", "ragc_debug_set_attn_plan", "ragc_debug_get_attn_plan",
            "ragc_debug_set_attn_product", "ragc_debug_get_attn_product"]
 
@@ -42,6 +43,11 @@ class ragc_batch(ctypes.Structure):
                 ("new_len", ctypes.c_void_p), ("new_start", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("h_prefix_len", ctypes.c_void_p), ("h_new_len", ctypes.c_void_p), ("h_new_start", ctypes.c_void_p),
                 ("h_block_table", ctypes.c_void_p)]
+
+
+class ragc_rope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class RagcError(RuntimeError):
@@ -84,6 +90,10 @@ def load() -> ctypes.CDLL:
         lib.ragc_debug_get_attn_product.argtypes = [P, P, I32, U32]
         lib.ragc_kv_append.restype = ctypes.c_int
         lib.ragc_kv_append.argtypes = [P, P, P, P, P]
+        lib.ragc_kv_append_rope.restype = ctypes.c_int
+        lib.ragc_kv_append_rope.argtypes = [P, P, P, P, P, P, P, P, I32, P]
+        lib.ragc_kv8_append.restype = ctypes.c_int
+        lib.ragc_kv8_append.argtypes = [P, P, P, P, P, P, P, I32, P]
         lib.ragc_kv_swap.restype = ctypes.c_int
         lib.ragc_kv_swap.argtypes = [P, P, P, I64, I32, P, P, I32, I32, U32, P]
         lib.ragc_kv_gather.restype = ctypes.c_int
@@ -115,10 +125,15 @@ def _check(rc: int) -> int:
     return rc
 
 
+def kv8_block_bytes(kv_heads: int, head_dim: int) -> int:
+    """One block of a plane of an 8-bit pool: tiles, a scale byte per head, padding to 16."""
+    return kv_heads * 16 * head_dim + -(-kv_heads // 16) * 16
+
+
 def make_pool(k, v, num_blocks: int, kv_heads: int, head_dim: int, dtype: int, block_stride_elems: Optional[int] = None,
               block_size: int = 16) -> ragc_kv_pool:
     if block_stride_elems is None:
-        block_stride_elems = kv_heads * block_size * head_dim
+        block_stride_elems = kv8_block_bytes(kv_heads, head_dim) if dtype == RAGC_DTYPE_E4M3 else kv_heads * block_size * head_dim
     return ragc_kv_pool(_ptr(k), _ptr(v), num_blocks, block_size, kv_heads, head_dim, dtype, 0, block_stride_elems)
 
 
@@ -127,6 +142,11 @@ def make_batch(num_reqs: int, table_stride: int, prefix_len, new_len, new_start,
     """Device arrays + host copies.  The caller keeps every array alive while the struct is used."""
     return ragc_batch(num_reqs, table_stride, _ptr(prefix_len), _ptr(new_len), _ptr(new_start), _ptr(block_table),
                       _ptr(h_prefix_len), _ptr(h_new_len), _ptr(h_new_start), _ptr(h_block_table))
+
+
+def make_rope(cos_sin, positions: int, rot_dim: int, interleaved: bool = False) -> ragc_rope:
+    """The caller keeps cos_sin alive while the struct is used."""
+    return ragc_rope(_ptr(cos_sin), positions, rot_dim, 1 if interleaved else 0, 0)
 
 
 def ragc_version() -> int:
@@ -183,6 +203,16 @@ def ragc_debug_get_attn_product(pool, batch, q_heads: int, flags: int = 0) -> in
 
 def ragc_kv_append(pool, batch, k_new, v_new, stream: int = 0) -> int:
     return _check(load().ragc_kv_append(_ref(pool), _ref(batch), _ptr(k_new), _ptr(v_new), stream or None))
+
+
+def ragc_kv_append_rope(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_heads: int, stream: int = 0) -> int:
+    return _check(load().ragc_kv_append_rope(_ref(pool), _ref(batch), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
+                                             _ptr(k_out), q_heads, stream or None))
+
+
+def ragc_kv8_append(pool, batch, rope, q, k_new, v_new, q_out, q_heads: int, stream: int = 0) -> int:
+    return _check(load().ragc_kv8_append(_ref(pool), _ref(batch), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
+                                         q_heads, stream or None))
 
 
 def ragc_kv_swap(pool, host_k, host_v, host_block_stride_elems: int, num_host_slots: int, dev_block_ids: np.ndarray,

@@ -1,0 +1,268 @@
+// Append to the 8-bit cache: e4m3 numbers with one power-of-two scale per block of 16 tokens, plane and kv head.
+//
+// Mathematics.  With amax the largest finite |x| of the tokens that join a block and e the smallest integer with amax <= 448 2^e
+// (448 is the largest e4m3 number), a number is stored as the e4m3 number nearest to x 2^-e, ties to even, and 2^e as the byte
+// e + 127 (at least 1).  A power of two costs nothing in relative precision, takes part in the attention's conversions
+// without a multiply, and lets a block be raised from e to a larger e' without a second rounding of any number that stays
+// normal: tokens that join a partly filled block take max(e_old, e_new), and only where that is above e_old are the stored ones
+// rounded anew.  Numbers that are not finite become NaN (0x7f; the type has no infinity) and leave the scale alone.
+//
+// K may be turned by its position first (kv_rope.h has the pairs).  That is done in fp64, where both products of a bf16 and
+// an fp32 number are exact, and comes down to fp32 with the last bit set where anything was lost (round to odd), so that the one
+// rounding that counts, to three bits of mantissa, is the correct one: the bytes are those of the definition.
+//
+// Layout, in the order in which the matrix cores take their operands: a K tile is [D/16][token][16], a V tile
+// [D/64][token/4][16][4][token%4] with element 64 i0 + 16 i3 + i2.
+//
+// Mapping.  A wave owns one (block, kv head), K and V: lane i has token i % 16 and the elements 16 c .. 16 c + 15 of every
+// fourth chunk c from i / 16 on.  V codes turn around in LDS.  Which block: item j of the launch belongs to the largest request
+// r with (new_start[r] - new_start[0] + 30 r) / 16 <= j, which leaves every request room for as many blocks as n tokens can touch
+// from any offset, (n + 30) / 16, so no list has to be made on the host and a captured launch follows the device arrays.
+#include "kv_rope.h"
+
+namespace ragc {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+constexpr int kCodeNan = 0x7f;
+
+// |x| of a finite number as a whole number that keeps its order and whether it lies above a border of 20 bits
+__device__ __forceinline__ uint32_t size_key(double x) {
+    const uint64_t b = __double_as_longlong(x);
+    const uint32_t hi = (uint32_t)(b >> 32) & 0x7fffffffu;
+    return hi >= 0x7ff00000u ? 0u : hi << 1 | ((uint32_t)b != 0);
+}
+// e + 127 for the largest key
+__device__ __forceinline__ int scale_byte(uint32_t key) {
+    const int e = (int)(key >> 21) - 1023 - 8 + ((key & 0x1fffff) > 0x180000u);  // 448 = 1.75 * 2^8
+    return key == 0 ? 1 : max(1, min(254, e + 127));
+}
+// fp64 to fp32 towards zero, with the last bit set where something was lost
+__device__ __forceinline__ float round_to_odd(double x) {
+    const float f = (float)x;
+    const double back = (double)f;
+    uint32_t u = __float_as_uint(f);
+    if (back != x) u = (__builtin_fabs(back) > __builtin_fabs(x) ? u - 1 : u) | 1;
+    return __uint_as_float(u);
+}
+// four numbers of at most 448, or not finite, to codes
+__device__ __forceinline__ uint32_t encode4(const float* x) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], v, true);
+    uint32_t u = (uint32_t)v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(__builtin_fabsf(x[i]) <= 448.f)) u = (u & ~(0xffu << 8 * i)) | (uint32_t)kCodeNan << 8 * i;
+    return u;
+}
+// codes of a scale 2^by times the new one, rounded to that
+__device__ __forceinline__ uint32_t raise4(uint32_t codes, int by) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    const float x[4] = {__builtin_ldexpf(a[0], by), __builtin_ldexpf(a[1], by), __builtin_ldexpf(b[0], by), __builtin_ldexpf(b[1], by)};
+    return encode4(x);
+}
+
+template <int D>
+__device__ __forceinline__ void append_block(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, int item, int head, char* lds) {
+    constexpr int NC = D / 64;  // 16-element chunks per lane
+    const int lane = threadIdx.x & 63, tok = lane & 15, cq = lane >> 4;
+    const int first_row = b.new_start[0];
+    // ---- which block of which request
+    auto first_item = [&](int start, int r) { return (start - first_row + 30 * r) >> 4; };
+    int r, start, prefix, n;
+    if (b.num_reqs <= 64) {
+        const int mine = min(lane, b.num_reqs - 1);
+        const int starts = b.new_start[mine], prefixes = b.prefix_len[mine], news = b.new_len[mine];
+        const uint64_t below = __builtin_amdgcn_ballot_w64(lane < b.num_reqs && first_item(starts, lane) <= item);
+        r = 63 - __builtin_clzll(below);
+        start = __builtin_amdgcn_readlane(starts, r);
+        prefix = __builtin_amdgcn_readlane(prefixes, r);
+        n = __builtin_amdgcn_readlane(news, r);
+    } else {
+        int lo = 0, hi = b.num_reqs;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first_item(b.new_start[mid], mid) <= item) lo = mid; else hi = mid;
+        }
+        r = lo;
+        start = b.new_start[r];
+        prefix = b.prefix_len[r];
+        n = b.new_len[r];
+    }
+    const int p = item - first_item(start, r), offset = prefix & (kBlock - 1);
+    if (n == 0 || p * kBlock >= offset + n) return;  // fewer blocks than there is room for
+    const int have = p == 0 ? offset : 0;            // tokens the block holds already
+    const int i0 = p == 0 ? 0 : p * kBlock - offset;  // first new token of the block
+    const int end = min(kBlock, have + n - i0);
+    const bool fresh = tok >= have && tok < end;
+    const int blk = b.block_table[(long long)r * b.table_stride + (prefix >> 4) + p];
+    const long long row = start + i0 + max(tok, have) - have < start + n ? start + i0 + max(tok, have) - have : start + n - 1;
+    const __bf16* const src_k = static_cast<const __bf16*>(x.k_new) + (row * b.kv_heads + head) * D;
+    const __bf16* const src_v = static_cast<const __bf16*>(x.v_new) + (row * b.kv_heads + head) * D;
+    const float* const angles = rope.cos_sin + (long long)(prefix + (int)(row - start)) * rope.rot_dim;
+    const int rot = rope.rot_dim, half = rot / 2;  // 0: nothing turns
+
+    double k[NC][16];
+    bf16x8 v[NC][2];
+    uint32_t key_k = 0, key_v = 0;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int d0 = (cq + 4 * c) * 16 + h * 8;
+            v[c][h] = *reinterpret_cast<const bf16x8*>(src_v + d0);
+            const bf16x8 own = *reinterpret_cast<const bf16x8*>(src_k + d0);
+            double* const out = k[c] + h * 8;
+            if (d0 >= rot) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = (double)(float)own[i];
+            } else if (rope.interleaved) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double cs = angles[d0 / 2 + i], sn = angles[half + d0 / 2 + i];
+                    const double a = (double)(float)own[2 * i], e = (double)(float)own[2 * i + 1];
+                    out[2 * i] = __builtin_fma(a, cs, -(e * sn));
+                    out[2 * i + 1] = __builtin_fma(a, sn, e * cs);
+                }
+            } else {
+                const bool first = d0 < half;
+                const bf16x8 other = *reinterpret_cast<const bf16x8*>(src_k + (first ? d0 + half : d0 - half));
+                const float* const at = angles + (first ? d0 : d0 - half);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double cs = at[i], sn = first ? -at[half + i] : at[half + i];
+                    out[i] = __builtin_fma((double)(float)own[i], cs, (double)(float)other[i] * sn);
+                }
+            }
+            if (fresh) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    key_k = max(key_k, size_key(out[i]));
+                    key_v = max(key_v, size_key((double)(float)v[c][h][i]));
+                }
+            }
+        }
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) {
+        key_k = max(key_k, (uint32_t)__shfl_xor((int)key_k, step, 64));
+        key_v = max(key_v, (uint32_t)__shfl_xor((int)key_v, step, 64));
+    }
+
+    uint8_t* const base_k = static_cast<uint8_t*>(x.pool_k) + (long long)blk * b.block_stride;
+    uint8_t* const base_v = static_cast<uint8_t*>(x.pool_v) + (long long)blk * b.block_stride;
+    uint8_t* const scale_k = base_k + (long long)b.kv_heads * (kBlock * D) + head;
+    uint8_t* const scale_v = base_v + (long long)b.kv_heads * (kBlock * D) + head;
+    uint8_t* const tile_k = base_k + (long long)head * (kBlock * D);
+    uint8_t* const tile_v = base_v + (long long)head * (kBlock * D);
+    int sk = scale_byte(key_k), sv = scale_byte(key_v);
+    int old_k = sk, old_v = sv;
+    if (have > 0) {
+        old_k = *scale_k;
+        old_v = *scale_v;
+        sk = max(sk, old_k);
+        sv = max(sv, old_v);
+    }
+
+    // ---- K: a 16-byte piece per token and chunk
+    const double down_k = __longlong_as_double((long long)(1023 + 127 - sk) << 52);
+    const bool again_k = sk != old_k && tok < have;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        u32x4* const to = reinterpret_cast<u32x4*>(tile_k + c * 1024 + lane * 16);
+        u32x4 codes;
+        if (fresh) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = round_to_odd(k[c][w * 4 + i] * down_k);
+                codes[w] = encode4(y);
+            }
+        }
+        if (again_k) {
+            const u32x4 was = *to;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) codes[w] = raise4(was[w], old_k - sk);
+        }
+        if (fresh || again_k) *to = codes;
+    }
+
+    // ---- V: the codes turn around in LDS, [token][element] with 4 bytes behind each row
+    constexpr int LROW = D + 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf((float)v[c][w >> 1][(w & 1) * 4 + i], 127 - sv);
+            *reinterpret_cast<uint32_t*>(lds + tok * LROW + (cq + 4 * c) * 16 + w * 4) = encode4(y);
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
+    const int t4 = cq * 4;  // this lane's four tokens, element 64 c + 16 w + lane % 16
+    uint32_t mask = 0, held = 0;  // bytes of new tokens, of tokens that are there
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (t4 + i >= have && t4 + i < end) mask |= 0xffu << 8 * i;
+        if (t4 + i < have) held |= 0xffu << 8 * i;
+    }
+    const bool again_v = sv != old_v && held != 0;
+    if (mask != 0 || again_v) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            u32x4* const to = reinterpret_cast<u32x4*>(tile_v + c * 1024 + lane * 16);
+            u32x4 codes;
+            if (mask != 0xffffffffu) codes = *to;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t u = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u |= (uint32_t)(uint8_t)lds[(t4 + i) * LROW + c * 64 + w * 16 + tok] << 8 * i;
+                if (mask != 0xffffffffu) {
+                    const uint32_t was = again_v ? (raise4(codes[w], old_v - sv) & held) | (codes[w] & ~held) : codes[w];
+                    u = (u & mask) | (was & ~mask);
+                }
+                codes[w] = u;
+            }
+            *to = codes;
+        }
+    }
+    if (lane == 0) {
+        *scale_k = (uint8_t)sk;
+        *scale_v = (uint8_t)sv;
+    }
+}
+
+constexpr int kWaves = 4;
+constexpr int kTurnHeads = 4;
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves) void kv8_append_kernel(PagedBatch b, RopeArgs rope, RopeRows x, int block_groups, int head_groups, int rows, int q_groups) {
+    __shared__ __attribute__((aligned(16))) char lds[kWaves][kBlock * (D + 4)];
+    if ((int)blockIdx.x < block_groups) {
+        const int w = threadIdx.x >> 6;
+        const int head = (int)blockIdx.x % head_groups * kWaves + w;
+        if (head < b.kv_heads) append_block<D>(b, rope, x, __builtin_amdgcn_readfirstlane((int)blockIdx.x / head_groups), __builtin_amdgcn_readfirstlane(head), lds[w]);
+        return;
+    }
+    const int id = (int)blockIdx.x - block_groups;
+    rope_rows<__bf16, kTurnHeads>(b, rope, x, 0, id / q_groups * rows, id % q_groups);
+}
+
+}  // namespace
+
+hipError_t launch_kv8_append(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, hipStream_t s) {
+    const int head_groups = (b.kv_heads + kWaves - 1) / kWaves;
+    const long long items = ((long long)x.total_new + 30LL * b.num_reqs) >> 4;
+    const int rows = 256 / (b.head_dim * 2 / 32), q_groups = (x.q_heads + kTurnHeads - 1) / kTurnHeads;
+    const long long blocks = items * head_groups, turns = (long long)((x.total_new + rows - 1) / rows) * q_groups;
+    if (blocks + turns > 0xffffff) return hipErrorInvalidValue;  // grid times workgroup size stays below 2^32 threads
+    const dim3 grid((unsigned)(blocks + turns)), block(64 * kWaves);
+    if (b.head_dim == 64) hipLaunchKernelGGL((kv8_append_kernel<64>), grid, block, 0, s, b, rope, x, (int)blocks, head_groups, rows, q_groups);
+    else hipLaunchKernelGGL((kv8_append_kernel<128>), grid, block, 0, s, b, rope, x, (int)blocks, head_groups, rows, q_groups);
+    return hipGetLastError();
+}
+
+}  // namespace ragc

@@ -4,23 +4,10 @@
 // helper), and whole-block copies between the device pool and a host-mapped
 // pinned pool (Sec. 5.1 "Swap out only once").  All three are HBM- or
 // host-link-bound copies in 16-byte units; values are never interpreted.
-#include "ragc_internal.h"
+#include "kv_rows.h"
 
 namespace ragc {
 namespace {
-
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-
-// Request that owns packed row t: largest r with new_start[r] <= t (new_start is
-// increasing and new_start[0] <= t < new_start[num_reqs]).
-__device__ __forceinline__ int find_request(const int32_t* __restrict__ new_start, int num_reqs, int t) {
-    int lo = 0, hi = num_reqs;  // invariant: new_start[lo] <= t < new_start[hi]
-    while (hi - lo > 1) {
-        int mid = (lo + hi) >> 1;
-        if (new_start[mid] <= t) lo = mid; else hi = mid;
-    }
-    return lo;
-}
 
 // Append.  A workgroup owns 16 consecutive packed rows (tokens) and a run of kv heads: 1024
 // 16-byte chunks per plane, four of K and four of V per thread, all loads issued before the
@@ -51,25 +38,9 @@ __global__ __launch_bounds__(256, 8) void append_kernel(PagedBatch b, char* __re
     const int head_bytes = b.head_dim * esize;
     const int lane = threadIdx.x & 63;
     const int t = first_row + t0 + min(lane & (kAppendRows - 1), rows - 1);
-    int r, start, prefix;
-    if (b.num_reqs <= 64) {  // one request per lane, then find_request among the lanes
-        const int mine = min(lane, b.num_reqs - 1);
-        const int starts = b.new_start[mine], prefixes = b.prefix_len[mine];
-        r = 0;
-#pragma unroll
-        for (int step = 32; step > 0; step >>= 1) {
-            const int s = __shfl(starts, r + step, 64);  // r + step <= 63
-            if (r + step < b.num_reqs && s <= t) r += step;
-        }
-        start = __shfl(starts, r, 64);
-        prefix = __shfl(prefixes, r, 64);
-    } else {
-        r = find_request(b.new_start, b.num_reqs, t);
-        start = b.new_start[r];
-        prefix = b.prefix_len[r];
-    }
-    const int pos = prefix + (t - start);
-    const int blk = b.block_table[(long long)r * b.table_stride + (pos >> 4)];
+    const RowAt at = locate_row(b, t);
+    const int pos = at.prefix + (t - at.start);
+    const int blk = b.block_table[(long long)at.req * b.table_stride + (pos >> 4)];
     // chunks per head is 8, 16 or 32 (head_dim 64 or 128, 2 or 4 bytes per element)
     const int cph_shift = __ffs(head_bytes >> 4) - 1;
     const int per_head_shift = cph_shift + 4;  // chunks of one head over the 16 rows

@@ -40,19 +40,29 @@ int esize_of(int32_t dtype) { return dtype == RAGC_DTYPE_BF16 ? 2 : dtype == RAG
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int check_pool(const ragc_kv_pool* pool) {
+// Bytes of one block of a plane of an 8-bit pool: the tiles, then a scale byte per kv head, to the next multiple of 16.
+int64_t kv8_block_bytes(const ragc_kv_pool* pool) {
+    return (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim + ((int64_t)pool->kv_heads + 15) / 16 * 16;
+}
+
+// eight_bit: 1 = an 8-bit pool is required, 0 = none is accepted, -1 = either
+int check_pool(const ragc_kv_pool* pool, int eight_bit = 0) {
     if (!pool) return fail(RAGC_ERR_NULL, "pool is NULL");
     if (!pool->k || !pool->v) return fail(RAGC_ERR_NULL, "pool->k / pool->v is NULL");
     if (pool->block_size != RAGC_BLOCK_SIZE) return fail(RAGC_ERR_SHAPE, "block_size %d (must be 16)", pool->block_size);
     if (pool->head_dim != 64 && pool->head_dim != 128) return fail(RAGC_ERR_SHAPE, "head_dim %d (must be 64 or 128)", pool->head_dim);
-    if (esize_of(pool->dtype) == 0) return fail(RAGC_ERR_SHAPE, "dtype %d unknown", pool->dtype);
+    const bool is8 = pool->dtype == RAGC_DTYPE_E4M3;
+    if (!is8 && esize_of(pool->dtype) == 0) return fail(RAGC_ERR_SHAPE, "dtype %d unknown", pool->dtype);
+    if (is8 && eight_bit == 0) return fail(RAGC_ERR_SHAPE, "an 8-bit pool: this call takes fp32 and bf16 ones (see ragc_kv8_append, ragc_kv8_attn)");
+    if (!is8 && eight_bit == 1) return fail(RAGC_ERR_SHAPE, "dtype %d: this call takes 8-bit pools (RAGC_DTYPE_E4M3)", pool->dtype);
     if (pool->reserved != 0) return fail(RAGC_ERR_SHAPE, "pool->reserved must be 0");
     if (pool->kv_heads <= 0 || pool->kv_heads > 65535) return fail(RAGC_ERR_SHAPE, "kv_heads %d", pool->kv_heads);
     if (pool->num_blocks <= 0) return fail(RAGC_ERR_SHAPE, "num_blocks %d", pool->num_blocks);
-    const int64_t min_stride = (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim;
+    const int64_t min_stride = is8 ? kv8_block_bytes(pool) : (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim;
     if (pool->block_stride_elems < min_stride)
-        return fail(RAGC_ERR_SHAPE, "block_stride_elems %lld < kv_heads*16*head_dim = %lld", (long long)pool->block_stride_elems, (long long)min_stride);
-    if (!aligned16(pool->k) || !aligned16(pool->v) || (pool->block_stride_elems * esize_of(pool->dtype)) % 16 != 0)
+        return fail(RAGC_ERR_SHAPE, "block_stride_elems %lld < %s = %lld", (long long)pool->block_stride_elems,
+                    is8 ? "kv_heads*16*head_dim + kv_heads, to the next 16," : "kv_heads*16*head_dim", (long long)min_stride);
+    if (!aligned16(pool->k) || !aligned16(pool->v) || (pool->block_stride_elems * (is8 ? 1 : esize_of(pool->dtype))) % 16 != 0)
         return fail(RAGC_ERR_ALIGN, "pool planes and block stride must be 16-byte aligned");
     return RAGC_OK;
 }
@@ -587,6 +597,59 @@ int prefill_attn_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const v
     return run_bf16_plan(a, h, plan, s);
 }
 
+int check_rope(const ragc_rope* rope, const ragc_kv_pool* pool) {
+    if (!rope->cos_sin) return fail(RAGC_ERR_NULL, "rope->cos_sin is NULL");
+    if (rope->rot_dim < 16 || rope->rot_dim > pool->head_dim || rope->rot_dim % 16 != 0)
+        return fail(RAGC_ERR_SHAPE, "rot_dim %d (a multiple of 16, 16 to head_dim)", rope->rot_dim);
+    if (rope->positions <= 0) return fail(RAGC_ERR_SHAPE, "rope->positions %d", rope->positions);
+    if (rope->interleaved != 0 && rope->interleaved != 1) return fail(RAGC_ERR_SHAPE, "rope->interleaved %d (0 or 1)", rope->interleaved);
+    if (rope->reserved != 0) return fail(RAGC_ERR_SHAPE, "rope->reserved must be 0");
+    if (!aligned16(rope->cos_sin)) return fail(RAGC_ERR_ALIGN, "rope->cos_sin must be 16-byte aligned");
+    return RAGC_OK;
+}
+
+// `out` is `in`, or the two do not overlap
+int check_in_place(const void* in, const void* out, int64_t bytes, const char* what) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(out);
+    if (a != b && a < b + (uintptr_t)bytes && b < a + (uintptr_t)bytes) return fail(RAGC_ERR_SHAPE, "%s overlaps its input without being it", what);
+    return RAGC_OK;
+}
+
+// Both appends with a rotation; an 8-bit pool takes bf16 rows and may come without one.
+int append_rope_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
+                     const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream) {
+    const bool is8 = pool->dtype == RAGC_DTYPE_E4M3;
+    const int es = is8 ? 2 : esize_of(pool->dtype);
+    if (rope)
+        if (int rc = check_rope(rope, pool)) return rc;
+    if (q_heads < 0 || q_heads % pool->kv_heads != 0)
+        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+    BatchInfo info;
+    HostMeta h;
+    if (int rc = check_batch(pool, batch, true, false, &h, &info)) return rc;
+    if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
+    if (int rc = check_packed(batch, h)) return rc;
+    if (rope)
+        for (int r = 0; r < batch->num_reqs; ++r)
+            if (h.new_len[r] > 0 && (int64_t)h.prefix_len[r] + h.new_len[r] > rope->positions)
+                return fail(RAGC_ERR_RANGE, "request %d: position %lld, rope->positions is %d", r, (long long)h.prefix_len[r] + h.new_len[r] - 1, rope->positions);
+    if (!k_new || !v_new) return fail(RAGC_ERR_NULL, "k_new / v_new is NULL");
+    if (q_heads > 0 ? !q || !q_out : q || q_out) return fail(RAGC_ERR_NULL, "q and q_out come together, with q_heads above 0, or not at all");
+    for (const void* p : {q, k_new, v_new, static_cast<const void*>(q_out), static_cast<const void*>(k_out)})
+        if (!aligned16(p)) return fail(RAGC_ERR_ALIGN, "q / k_new / v_new / q_out / k_out must be 16-byte aligned");
+    const int64_t head_bytes = ((int64_t)h.new_start[0] + info.total_new) * pool->head_dim * es;
+    if (int rc = check_in_place(q, q_out, q_heads * head_bytes, "q_out")) return rc;
+    if (k_out)
+        if (int rc = check_in_place(k_new, k_out, pool->kv_heads * head_bytes, "k_out")) return rc;
+    const ragc::RopeArgs args = {rope ? rope->cos_sin : nullptr, rope ? rope->rot_dim : 0, rope ? rope->interleaved : 0};
+    const ragc::RopeRows rows = {q, k_new, v_new, q_out, k_out, pool->k, pool->v, q_heads, (int32_t)info.total_new};
+    const ragc::PagedBatch pb = make_paged(pool, batch);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = is8 ? ragc::launch_kv8_append(pb, args, rows, s) : ragc::launch_append_rope(pb, args, rows, es, s);
+    if (e != hipSuccess) return hip_fail(e, "append launch");
+    return RAGC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -713,6 +776,22 @@ int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void
     return RAGC_OK;
 }
 
+int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
+                        const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream) {
+    g_err[0] = 0;
+    if (int rc = check_pool(pool)) return rc;
+    if (!rope) return fail(RAGC_ERR_NULL, "rope is NULL (ragc_kv_append stores rows as they are)");
+    return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_heads, stream);
+}
+
+int ragc_kv8_append(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
+                    const void* v_new, void* q_out, int32_t q_heads, void* stream) {
+    g_err[0] = 0;
+    if (int rc = check_pool(pool, 1)) return rc;
+    if (!rope && (q || q_out || q_heads != 0)) return fail(RAGC_ERR_SHAPE, "q without a rope: nothing would be done to it");
+    return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, nullptr, q_heads, stream);
+}
+
 int ragc_kv_gather(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t req, int32_t length, void* k_out,
                    void* v_out, void* stream) {
     g_err[0] = 0;
@@ -741,13 +820,15 @@ int ragc_kv_swap(const ragc_kv_pool* pool, void* host_k, void* host_v, int64_t h
                  int32_t num_host_slots, const int32_t* dev_block_ids, const int32_t* host_slots, int32_t n,
                  int32_t direction, uint32_t flags, void* stream) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool)) return rc;
+    if (int rc = check_pool(pool, -1)) return rc;
     if (!host_k || !host_v) return fail(RAGC_ERR_NULL, "host_k / host_v is NULL");
     if (n < 0) return fail(RAGC_ERR_RANGE, "n %d", n);
     if (direction != RAGC_SWAP_TO_DEVICE && direction != RAGC_SWAP_TO_HOST) return fail(RAGC_ERR_SHAPE, "direction %d", direction);
     if (flags > RAGC_SWAP_KERNEL) return fail(RAGC_ERR_SHAPE, "unknown swap flags 0x%x", flags);
-    const int es = esize_of(pool->dtype);
-    const int64_t plane_elems = (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim;
+    const bool is8 = pool->dtype == RAGC_DTYPE_E4M3;
+    const int es = is8 ? 1 : esize_of(pool->dtype);
+    // a block of an 8-bit pool takes its scales along
+    const int64_t plane_elems = is8 ? kv8_block_bytes(pool) : (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim;
     if (host_block_stride_elems < plane_elems)
         return fail(RAGC_ERR_SHAPE, "host_block_stride_elems %lld < %lld", (long long)host_block_stride_elems, (long long)plane_elems);
     if (!aligned16(host_k) || !aligned16(host_v) || (host_block_stride_elems * es) % 16 != 0)

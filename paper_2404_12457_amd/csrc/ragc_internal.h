@@ -118,6 +118,28 @@ hipError_t launch_attn_bf16_merge(const AttnLaunch& a, const AttnWork& wk, int e
 
 hipError_t launch_append(const PagedBatch& b, void* pool_k, void* pool_v, const void* k_new, const void* v_new,
                          int32_t total_new, int esize, hipStream_t s);
+
+// Position rotation (kv_rope.h): angles of position p in row p of cos_sin, rot_dim/2 cos and as many sin.
+struct RopeArgs {
+    const float* cos_sin;
+    int32_t rot_dim;  // 0: nothing turns
+    int32_t interleaved;
+};
+// Packed rows of the new tokens and where they go; q_out may be q and k_out k_new; q_heads = 0: no Q, k_out NULL: the pool only.
+struct RopeRows {
+    const void* q;
+    const void* k_new;
+    const void* v_new;
+    void* q_out;
+    void* k_out;
+    void* pool_k;
+    void* pool_v;
+    int32_t q_heads;
+    int32_t total_new;
+};
+hipError_t launch_append_rope(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, int esize, hipStream_t s);
+// 8-bit pool, bf16 rows; block_stride in bytes
+hipError_t launch_kv8_append(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, hipStream_t s);
 hipError_t launch_gather(const PagedBatch& b, int32_t req, int32_t length, void* k_out, void* v_out, int esize,
                          hipStream_t s);
 

@@ -1,0 +1,226 @@
+"""GPU parity of the append with position rotation and of the 8-bit cache against the oracle in 64 bits."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import kv8 as O
+from paper_2404_12457_amd import binding as B
+
+from kv8_util import Case
+
+pytestmark = pytest.mark.gpu
+
+ODD = [(0, 1), (5, 1), (15, 1), (15, 2), (16, 16), (3, 40), (0, 0), (31, 0), (100, 133), (47, 17), (16, 1), (0, 64)]
+STEPS = [(int(p), 1) for p in np.random.Generator(np.random.PCG64(1)).integers(0, 400, 70)]  # more requests than a wave has lanes
+HALF_STEP = {"bf16": 2.0**-8, "f32": 2.0**-24}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load()
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _rope(c, rot_dim, interleaved):
+    cs = O.angles(int((c.h_prefix + c.h_new).max()), rot_dim)
+    dev = torch.from_numpy(cs).cuda()
+    return cs, dev, B.make_rope(dev, len(cs), rot_dim, interleaved)
+
+
+def _near(got, want, sides, dtype):
+    """One rounding to the type, and in fp32 one of a product and one of the sum."""
+    off = np.abs(got - want) - (HALF_STEP[dtype] * np.abs(want) * 1.001 + 2.0**-23 * sides + 1e-38)
+    worst = float(off.max())
+    assert worst <= 0
+
+
+def _sides(x, cs, interleaved, c):
+    """|a cos| + |b sin| for the first of each turned pair, |a sin| + |b cos| for the second, |x| elsewhere.  The first is
+    |a| |cos| - |b| (-|sin|), the first element of |x| turned by (|cos|, -|sin|); the second that of |x| turned by (|cos|, |sin|).
+    What these two turns give for the other element of the pair is a difference of the same sides, no larger than they are."""
+    half = cs.shape[1] // 2
+    minus = np.abs(cs) * np.concatenate([np.ones(half), -np.ones(half)]).astype(np.float32)
+    return np.maximum(c.rotated(np.abs(x), minus, interleaved), c.rotated(np.abs(x), np.abs(cs), interleaved))
+
+
+@pytest.mark.parametrize("lens", [ODD, STEPS, [(7, 1)], [(0, 515)]], ids=["odd", "steps", "one", "prompt"])
+@pytest.mark.parametrize("dtype,hq,hkv,d,rot,inter", [("bf16", 8, 2, 128, 128, False), ("bf16", 6, 3, 64, 16, False), ("bf16", 5, 5, 128, 64, True),
+                                                     ("f32", 4, 2, 64, 32, True), ("f32", 3, 1, 128, 128, False), ("f32", 7, 7, 64, 48, False)])
+def test_append_rope(lens, dtype, hq, hkv, d, rot, inter):
+    c = Case(lens, hq, hkv, d, dtype, seed=hq, pad=hkv % 2, first_row=3)
+    cs, keep, rope = _rope(c, rot, inter)
+    q, k, v = (c.host(t) for t in (c.q, c.k_new, c.v_new))
+    before = [c.host(p) for p in c.planes]
+    q_out, k_out = torch.full_like(c.q, 7.0), torch.full_like(c.k_new, 7.0)
+    B.ragc_kv_append_rope(c.pool, c.batch, rope, c.q, c.k_new, c.v_new, q_out, k_out, hq, _stream())
+    torch.cuda.synchronize()
+    tol = [_sides(x, cs, inter, c)[3:] for x in (q, k)]
+    qr, kr = c.rotated(q, cs, inter), c.rotated(k, cs, inter)
+    _near(c.host(q_out)[3:], qr[3:], tol[0], dtype)
+    _near(c.host(k_out)[3:], kr[3:], tol[1], dtype)
+    assert torch.all(q_out[:3] == 7) and torch.all(k_out[:3] == 7)  # rows before the first are not the call's
+    # the pool has the very rows of k_out and v_new, and nothing else has changed
+    want = [b.copy() for b in before]
+    for plane, rows in zip(want, (c.host(k_out), v)):
+        tiles = plane[:, :hkv * 16 * d].reshape(-1, hkv, 16, d)
+        for r, p, n, at in c.spans():
+            pos = np.arange(p, p + n)
+            tiles[c.h_table[r, pos // 16], :, pos % 16] = rows[at]
+        plane[:, :hkv * 16 * d] = tiles.reshape(len(plane), -1)
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(c.host(got), w)
+    # in place, and the same bits
+    q2, k2 = c.q.clone(), c.k_new.clone()
+    B.ragc_kv_append_rope(c.pool, c.batch, rope, q2, k2, c.v_new, q2, k2, hq, _stream())
+    assert torch.equal(q2[3:], q_out[3:]) and torch.equal(k2[3:], k_out[3:])
+    # without Q and without the copy of K
+    B.ragc_kv_append_rope(c.pool, c.batch, rope, None, c.k_new, c.v_new, None, None, 0, _stream())
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(c.host(got), w)
+
+
+@pytest.mark.parametrize("lens", [ODD, STEPS, [(7, 1)], [(0, 515)]], ids=["odd", "steps", "one", "prompt"])
+@pytest.mark.parametrize("hq,hkv,d,rot,inter", [(8, 2, 128, 128, False), (6, 3, 64, 16, False), (5, 5, 128, 64, True), (9, 9, 64, 48, False), (0, 17, 64, 0, False)])
+def test_kv8_append_gives_the_bytes_of_the_definition(lens, hq, hkv, d, rot, inter):
+    c = Case(lens, max(hq, 1), hkv, d, seed=hkv, pad=hkv % 2, first_row=5)
+    k, v, q = (c.host(t) for t in (c.k_new, c.v_new, c.q))
+    q_out = torch.full_like(c.q, 7.0)
+    cs, keep, rope = _rope(c, rot, inter) if rot else (None, None, None)
+    want = c.appended8(c.rotated(k, cs, inter) if rot else k, v)
+    B.ragc_kv8_append(c.pool, c.batch, rope, c.q if hq else None, c.k_new, c.v_new, q_out if hq else None, hq, _stream())
+    torch.cuda.synchronize()
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    if hq:
+        _near(c.host(q_out)[5:], c.rotated(q, cs, inter)[5:], _sides(q, cs, inter, c)[5:], "bf16")
+    assert torch.all(q_out[:5 if hq else None] == 7)
+    # a second time: the tokens are there, the scales hold them, nothing changes
+    B.ragc_kv8_append(c.pool, c.batch, rope, None, c.k_new, c.v_new, None, 0, _stream())
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(got.cpu().numpy(), w)
+
+
+def test_kv8_append_token_by_token_raises_scales_as_the_definition_says():
+    """40 single tokens, each larger than the last by a random factor, so that blocks are rounded anew again and again."""
+    c = Case([(0, 40), (9, 40)], 2, 2, 64, seed=3)
+    grow = torch.from_numpy(np.exp2(np.cumsum(c.rng.uniform(0, 1.5, 40)) - 20).astype(np.float32)).cuda()
+    for t in (c.k_new, c.v_new):
+        t.mul_(torch.cat([grow, grow])[:, None, None].to(t.dtype))
+    start = c.h_prefix.copy()
+    for i in range(40):
+        hp, hn, hs = (start + i).astype(np.int32), np.ones(2, np.int32), np.arange(3, dtype=np.int32)
+        rows = torch.tensor([i, 40 + i], device="cuda")
+        k, v = c.k_new[rows].contiguous(), c.v_new[rows].contiguous()
+        want = []
+        for plane, is_k, x in zip(c.planes, (True, False), (k, v)):
+            b = plane.cpu().numpy().copy()
+            for r in range(2):
+                O.write_tokens(b, c.h_table[r], int(hp[r]), c.host(x)[r:r + 1], is_k)
+            want.append(b)
+        dev = [torch.from_numpy(a).cuda() for a in (hp, hn, hs)]
+        batch = B.make_batch(2, c.h_table.shape[1], *dev, c.dev[3], hp, hn, hs, c.h_table)
+        B.ragc_kv8_append(c.pool, batch, None, None, k, v, None, 0, _stream())
+        for got, w in zip(c.planes, want):
+            assert np.array_equal(got.cpu().numpy(), w), i
+
+
+def test_kv8_append_of_zeros_tiny_huge_and_what_is_not_finite():
+    c = Case([(0, 48), (6, 20)], 1, 2, 128, seed=4)
+    k = c.k_new.float()
+    k[0:16] = 0
+    k[16:32] *= 2.0**-130          # below the smallest scale: subnormal codes and zeros
+    k[32:48] *= 2.0**125
+    k[50, 0, :4] = torch.tensor([float("inf"), float("-inf"), float("nan"), 1.0])
+    k[55] = float("nan")           # a whole token
+    c.k_new.copy_(k)
+    c.v_new.copy_(k.flip(-1))
+    want = c.appended8(c.host(c.k_new), c.host(c.v_new))
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(got.cpu().numpy(), w)
+
+
+def test_appends_follow_the_device_arrays_when_a_graph_is_replayed():
+    """A decode step captured once: prefix_len moves on between the replays, new_len stays.  Every request has blocks of its
+    own for the tokens of all steps, as the calls require."""
+    c = Case([(p, 1) for p in (0, 14, 15, 100)], 8, 2, 128, seed=5, room=4)
+    t = Case([(p, 1) for p in (0, 14, 15, 100)], 8, 2, 128, "bf16", seed=5, room=4)
+    cs = O.angles(200, 128)
+    dev = torch.from_numpy(cs).cuda()
+    rope = B.make_rope(dev, 200, 128)
+    q_out = torch.empty_like(c.q)
+    tq, tk = torch.empty_like(t.q), torch.empty_like(t.k_new)
+
+    def calls(s):
+        B.ragc_kv8_append(c.pool, c.batch, rope, c.q, c.k_new, c.v_new, q_out, 8, s)
+        B.ragc_kv_append_rope(t.pool, t.batch, rope, t.q, t.k_new, t.v_new, tq, tk, 8, s)
+
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls(side.cuda_stream)
+    first = c.h_prefix.copy()
+    for step in range(4):
+        for x in (c, t):
+            x.h_prefix[:] = first + step
+            x.dev[0].copy_(torch.from_numpy(x.h_prefix))
+            for rows in (x.q, x.k_new, x.v_new):
+                rows.normal_()
+        want = c.appended8(c.rotated(c.host(c.k_new), cs, False), c.host(c.v_new))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip(c.planes, want):
+            assert np.array_equal(got.cpu().numpy(), w)
+        qr = c.rotated(c.host(c.q), cs, False)
+        _near(c.host(q_out), qr, _sides(c.host(c.q), cs, False, c), "bf16")
+        eager_q, eager_k = torch.empty_like(tq), torch.empty_like(tk)
+        pools = [p.clone() for p in t.planes]
+        B.ragc_kv_append_rope(t.pool, t.batch, rope, t.q, t.k_new, t.v_new, eager_q, eager_k, 8, _stream())
+        assert torch.equal(eager_q, tq) and torch.equal(eager_k, tk)
+        for a, b in zip(pools, t.planes):
+            assert torch.equal(a, b)
+
+
+def test_swap_moves_8_bit_blocks_with_their_scales():
+    c = Case([(64, 1)], 4, 3, 64, seed=6)
+    need = O.block_bytes(3, 64)
+    host = [torch.zeros(6, need, dtype=torch.uint8).pin_memory() for _ in range(2)]
+    before = [p.clone() for p in c.planes]
+    ids, slots = np.array([4, 1, 2], np.int32), np.array([0, 5, 3], np.int32)
+    for flags in (B.RAGC_SWAP_KERNEL, B.RAGC_SWAP_MEMCPY):
+        for x in host:
+            x.zero_()
+        B.ragc_kv_swap(c.pool, *host, need, 6, ids, slots, B.RAGC_SWAP_TO_HOST, flags, _stream())
+        torch.cuda.synchronize()
+        for h, b in zip(host, before):
+            assert torch.equal(h[slots.tolist()], b[ids.tolist(), :need].cpu()) and not h[[1, 2, 4]].any()
+        for p in c.planes:
+            p[ids.tolist()] = 0
+        B.ragc_kv_swap(c.pool, *host, need, 6, ids, slots, B.RAGC_SWAP_TO_DEVICE, flags, _stream())
+        torch.cuda.synchronize()
+        for p, b in zip(c.planes, before):
+            assert torch.equal(p, b)
+
+
+def test_append_rope_then_prefill_attention_is_attention_over_rotated_rows():
+    """The run of the two as a server uses them: turned in place, stored, then attended to."""
+    from oracle import attention as OA
+
+    c = Case([(40, 21), (0, 33), (130, 1)], 8, 2, 128, "bf16", seed=8)
+    cs, keep, rope = _rope(c, 128, False)
+    B.ragc_kv_append_rope(c.pool, c.batch, rope, c.q, c.k_new, c.v_new, c.q, c.k_new, 8, _stream())
+    out = torch.empty_like(c.q)
+    B.ragc_prefill_attn(c.pool, c.batch, c.q, c.k_new, c.v_new, out, 8, 128**-0.5, 0, None, 0, _stream())
+    torch.cuda.synchronize()
+    tiles = [c.host(p)[:, :2 * 16 * 128].reshape(-1, 2, 16, 128) for p in c.planes]
+    for r, p, n, rows in c.spans():
+        pos = np.arange(p + n)
+        k, v = (x[c.h_table[r, pos // 16], :, pos % 16] for x in tiles)
+        want = OA.prefill_attn(c.host(c.q)[rows], k, v, p, 128**-0.5)
+        assert np.max(np.abs(c.host(out)[rows] - want)) <= 2e-2

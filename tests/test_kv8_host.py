@@ -1,0 +1,180 @@
+"""Rotation and 8-bit cache without a GPU: the oracle against hand-worked and brute-force values, and the refusals of the
+entry points, which come before anything touches the device."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv8 as O
+from paper_2404_12457_amd import binding as B
+
+A = 0x10000  # a fake, aligned, non-NULL address: validation never dereferences device pointers
+FAR = 0x40000000
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    return B.load()
+
+
+# ---- the oracle -----------------------------------------------------------------------------
+def test_e4m3_values_and_rounding_by_hand():
+    assert O.VALUES[0x7E] == 448 and O.VALUES[0x01] == 2.0**-9 and O.VALUES[0x08] == 2.0**-6 and O.VALUES[0xB8] == -1.0
+    assert math.isnan(O.VALUES[0x7F]) and math.isnan(O.VALUES[0xFF])
+    x = np.array([448, 432, 431.9, 433, 1.0625, 1.1875, 2.0**-10, 1.01 * 2.0**-10, -0.0, np.inf, np.nan, -17.0])
+    want = [0x7E, 0x7E, 0x7D, 0x7E, 0x38, 0x3A, 0x00, 0x01, 0x80, 0x7F, 0x7F, 0xD8]  # 432, 1.0625 and 2^-10 are ties, -17 too
+    assert O.encode(x).tolist() == want
+    codes = np.array([c for c in range(256) if c & 0x7F != 0x7F], np.uint8)
+    assert np.array_equal(O.encode(O.VALUES[codes]), codes)
+
+
+def test_e4m3_rounding_against_torch():
+    torch = pytest.importorskip("torch")
+    x = np.random.Generator(np.random.PCG64(5)).standard_normal(20000).astype(np.float32) * 40
+    assert np.array_equal(O.encode(x.astype(np.float64)), torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy())
+
+
+@pytest.mark.parametrize("amax,want", [(0.0, 1), (448.0, 127), (448.0001, 128), (224.0, 126), (1.0, 119), (1.75, 119), (1.7500001, 120),
+                                       (3.3e38, 247), (2.0**-133, 1)])
+def test_scale_is_the_smallest_that_holds_the_largest_value(amax, want):
+    assert O.scale_byte(amax) == want
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tile_orders_are_permutations_with_the_documented_neighbours(d):
+    k, v = O.byte_of(d, True), O.byte_of(d, False)
+    assert np.array_equal(np.sort(k.ravel()), np.arange(16 * d)) and np.array_equal(np.sort(v.ravel()), np.arange(16 * d))
+    assert (k[0, :16] == np.arange(16)).all() and (k[:, 0] == 16 * np.arange(16)).all()
+    assert (v[:4, 0] == np.arange(4)).all() and (v[0, :64:16] == 4 * np.arange(4)).all() and (v[0, :16] == 16 * np.arange(16)).all()
+
+
+def test_a_raised_scale_leaves_normal_numbers_alone():
+    g = np.random.Generator(np.random.PCG64(6))
+    x = g.standard_normal((9, 1, 64))
+    plane = np.zeros((1, O.block_bytes(1, 64)), np.uint8)
+    O.write_tokens(plane, [0], 0, x, True)
+    before = O.read_tokens(plane, [0], 9, 1, 64, True)
+    O.write_tokens(plane, [0], 9, 30 * x[:1], True)
+    after = O.read_tokens(plane, [0], 10, 1, 64, True)
+    e = int(plane[0, 16 * 64]) - 127
+    normal = np.abs(before) >= 2.0 ** (e - 6)
+    assert np.array_equal(before[normal], after[:9][normal]) and np.abs(after[:9] - before).max() <= 2.0 ** (e - 10)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_keeps_lengths_and_relative_angles(interleaved):
+    g = np.random.Generator(np.random.PCG64(7))
+    cs = O.angles(50, 32)
+    x, y = g.standard_normal((2, 1, 1, 64))
+    dot = lambda p, q: float((O.rotate(x, p, cs, interleaved) * O.rotate(y, q, cs, interleaved)).sum())  # noqa: E731
+    assert abs(dot(40, 37) - dot(5, 2)) < 1e-5 and abs(dot(0, 0) - float((x * y).sum())) < 1e-12
+    assert np.array_equal(O.rotate(x, 9, cs, interleaved)[..., 32:], x[..., 32:])
+
+
+# ---- the refusals ---------------------------------------------------------------------------
+def _pool(dtype=B.RAGC_DTYPE_BF16, **kw):
+    args = dict(k=A, v=A, num_blocks=64, kv_heads=2, head_dim=128, dtype=dtype)
+    args.update(kw)
+    return B.make_pool(**args)
+
+
+def _pool8(**kw):
+    return _pool(B.RAGC_DTYPE_E4M3, **kw)
+
+
+def _batch(p=(10,), n=(5,), stride=4, table=None, dev=A, start=None):
+    hp, hn = np.asarray(p, np.int32), np.asarray(n, np.int32)
+    hs = np.concatenate([[0], np.cumsum(np.maximum(hn, 0))]).astype(np.int32) if start is None else np.asarray(start, np.int32)
+    b = B.make_batch(len(p), stride, dev, dev, dev, dev, hp, hn, hs, table)
+    b.keep = (hp, hn, hs, table)
+    return b
+
+
+def _rope(**kw):
+    args = dict(cos_sin=A, positions=64, rot_dim=128)
+    args.update(kw)
+    return B.make_rope(**args)
+
+
+def _code(f, *a):
+    with pytest.raises(B.RagcError) as e:
+        f(*a)
+    return e.value.code
+
+
+def _rope_code(pool=None, batch=None, rope=None, q=A, k=A, v=A, qo=A, ko=None, hq=8):
+    return _code(B.ragc_kv_append_rope, pool or _pool(), batch or _batch(), rope or _rope(), q, k, v, qo, ko, hq)
+
+
+def _append8_code(pool=None, batch=None, rope="", q=A, k=A, v=A, qo=A, hq=8):
+    return _code(B.ragc_kv8_append, pool or _pool8(), batch or _batch(), _rope() if rope == "" else rope, q, k, v, qo, hq)
+
+
+@pytest.mark.parametrize("code", [_rope_code, _append8_code])
+def test_appends_with_a_rotation_refuse(code):
+    r = _rope()
+    r.reserved = 1
+    assert code(rope=r) == B.RAGC_ERR_SHAPE
+    r = _rope()
+    r.interleaved = 2
+    assert code(rope=r) == B.RAGC_ERR_SHAPE
+    assert code(rope=_rope(cos_sin=None)) == B.RAGC_ERR_NULL
+    assert code(rope=_rope(cos_sin=A + 4)) == B.RAGC_ERR_ALIGN
+    for rot in (0, -16, 8, 24, 144):
+        assert code(rope=_rope(rot_dim=rot)) == B.RAGC_ERR_SHAPE
+    assert code(rope=_rope(positions=0)) == B.RAGC_ERR_SHAPE
+    assert code(rope=_rope(positions=14)) == B.RAGC_ERR_RANGE  # the last new token is at position 14
+    assert "position 14" in B.ragc_last_error()
+    assert code(hq=7) == B.RAGC_ERR_SHAPE and code(hq=-2) == B.RAGC_ERR_SHAPE
+    assert code(hq=0) == B.RAGC_ERR_NULL and code(q=None) == B.RAGC_ERR_NULL and code(qo=None) == B.RAGC_ERR_NULL
+    assert code(k=None) == B.RAGC_ERR_NULL and code(v=None) == B.RAGC_ERR_NULL
+    for name in ("q", "k", "v", "qo"):
+        assert code(**{name: A + 8}) == B.RAGC_ERR_ALIGN
+    assert code(qo=A + 256) == B.RAGC_ERR_SHAPE and "overlaps" in B.ragc_last_error()
+    assert code(batch=_batch(dev=None)) == B.RAGC_ERR_NULL
+    assert code(batch=_batch(p=(60,), n=(10,))) == B.RAGC_ERR_RANGE
+    assert code(batch=_batch(p=(-1,))) == B.RAGC_ERR_RANGE
+    assert code(batch=_batch(p=(1, 1), n=(5, 2), start=(0, 6, 8))) == B.RAGC_ERR_RANGE
+    assert code(batch=_batch(p=(20,), n=(5,), table=np.array([[1, 64, 0, 0]], np.int32))) == B.RAGC_ERR_RANGE
+
+
+def test_rope_append_refuses_what_is_its_own():
+    assert _rope_code(pool=_pool8()) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_kv_append_rope, _pool(), _batch(), None, A, A, A, A, None, 8) == B.RAGC_ERR_NULL
+    assert _rope_code(ko=A + 64) == B.RAGC_ERR_SHAPE
+    assert _rope_code(ko=FAR + 8) == B.RAGC_ERR_ALIGN
+
+
+def test_kv8_append_refuses_what_is_its_own():
+    for dtype in (B.RAGC_DTYPE_F32, B.RAGC_DTYPE_BF16, 3):
+        assert _append8_code(pool=_pool(dtype)) == B.RAGC_ERR_SHAPE
+    assert _append8_code(rope=None) == B.RAGC_ERR_SHAPE  # q without a rotation
+    assert _append8_code(rope=None, q=None, qo=None, hq=8) == B.RAGC_ERR_SHAPE
+    assert _append8_code(pool=_pool8(block_stride_elems=2 * 16 * 128 + 8)) == B.RAGC_ERR_SHAPE  # no room for the scales
+    assert _append8_code(pool=_pool8(block_stride_elems=2 * 16 * 128 + 24)) == B.RAGC_ERR_ALIGN
+    assert _append8_code(pool=_pool8(k=A + 8)) == B.RAGC_ERR_ALIGN
+
+
+def test_other_calls_refuse_an_8_bit_pool():
+    b = _batch()
+    assert _code(B.ragc_prefill_attn, _pool8(), b, A, A, A, A, 8, 0.1) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_prefill_attn_static, _pool8(), b, A, A, A, A, 8, 0.1) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_prefill_attn_workspace, _pool8(), b, 8) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_kv_append, _pool8(), b, A, A) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_kv_gather, _pool8(), b, 0, 4, A, A) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_debug_get_attn_plan, _pool8(), b, 8) == B.RAGC_ERR_SHAPE
+
+
+def test_empty_batches_are_nothing():
+    none = _batch(p=(10,), n=(0,))
+    assert B.ragc_kv_append_rope(_pool(), none, _rope(), None, None, None, None, None, 0) == 0
+    assert B.ragc_kv8_append(_pool8(), none, None, None, None, None, None, 0) == 0
+
+
+def test_swap_of_8_bit_pools_counts_the_scales():
+    need = B.kv8_block_bytes(2, 128)
+    assert need == 2 * 16 * 128 + 16 and B.kv8_block_bytes(17, 64) == 17 * 16 * 64 + 32
+    ids = np.zeros(1, np.int32)
+    assert _code(B.ragc_kv_swap, _pool8(), A, A, need - 16, 4, ids, ids, B.RAGC_SWAP_TO_HOST) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_kv_swap, _pool8(), A, A, need + 8, 4, ids, ids, B.RAGC_SWAP_TO_HOST) == B.RAGC_ERR_ALIGN
+    assert B.ragc_kv_swap(_pool8(), A, A, need, 4, np.zeros(0, np.int32), np.zeros(0, np.int32), B.RAGC_SWAP_TO_HOST) == 0
