@@ -320,6 +320,21 @@ int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const
 int ragc_kv8_append(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
                     const void* v_new, void* q_out, int32_t q_heads, void* stream);
 
+/* Workspace ragc_kv8_attn needs for this batch with these flags (bytes, often 0): long key ranges are divided among workgroups
+ * whose partial results pass through it, unless RAGC_ATTN_NO_SPLIT is given.  Only the host arrays of `batch` are read.
+ * Returns a negative ragc_status on error. */
+int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags);
+
+/* Attention of the new tokens of every request over an 8-bit pool, causal, for prompts and for single tokens:
+ *     out[t,h,:] = softmax_j( scale * q[t,h,:] . K_j ) V_j ,  j = 0 .. prefix_len+i
+ * with every K_j, V_j, those of the new tokens too, from the pool: ragc_kv8_append comes first, on the same stream.
+ * Arguments, workspace, lengths under capture and requests without new tokens as for ragc_prefill_attn; q and out are
+ * bf16, flags RAGC_ATTN_NO_SPLIT and RAGC_ATTN_VALIDATE.  Softmax and sums are fp32, probabilities are rounded to bf16
+ * before the product with V and the output to nearest even.  A key or value that a row does not see counts nothing
+ * there, whatever its bytes; NaN in one that it sees reaches it. */
+int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
+                  uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Copy whole blocks (all kv heads, K and V planes) between the device pool and a
  * pinned host pool of the same per-block layout (Sec. 5.1 "Swap out only once";
  * Sec. 3.2 "Cache hit": the transfer is part of the hit latency).

@@ -27,7 +27,7 @@ RAGC_SWAP_TO_DEVICE, RAGC_SWAP_TO_HOST = 0, 1
 
 EXPORTS = ["ragc_version", "ragc_last_error", "ragc_kv_bytes_per_token", "ragc_prefill_attn_workspace",
            "ragc_prefill_attn", "ragc_prefill_attn_static", "ragc_kv_append", "ragc_kv_swap", "ragc_kv_gather",
-           "ragc_kv_append_rope", "ragc_kv8_append",
+           "ragc_kv_append_rope", "ragc_kv8_append", "ragc_kv8_attn_workspace", "ragc_kv8_attn",
            "ragc_batch_validate", "ragc_debug_set_attn_plan", "ragc_debug_get_attn_plan",
            "ragc_debug_set_attn_product", "ragc_debug_get_attn_product"]
 
@@ -94,6 +94,10 @@ def load() -> ctypes.CDLL:
         lib.ragc_kv_append_rope.argtypes = [P, P, P, P, P, P, P, P, I32, P]
         lib.ragc_kv8_append.restype = ctypes.c_int
         lib.ragc_kv8_append.argtypes = [P, P, P, P, P, P, P, I32, P]
+        lib.ragc_kv8_attn_workspace.restype = I64
+        lib.ragc_kv8_attn_workspace.argtypes = [P, P, I32, U32]
+        lib.ragc_kv8_attn.restype = ctypes.c_int
+        lib.ragc_kv8_attn.argtypes = [P, P, P, P, I32, ctypes.c_float, U32, P, ctypes.c_size_t, P]
         lib.ragc_kv_swap.restype = ctypes.c_int
         lib.ragc_kv_swap.argtypes = [P, P, P, I64, I32, P, P, I32, I32, U32, P]
         lib.ragc_kv_gather.restype = ctypes.c_int
@@ -213,6 +217,16 @@ def ragc_kv_append_rope(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_head
 def ragc_kv8_append(pool, batch, rope, q, k_new, v_new, q_out, q_heads: int, stream: int = 0) -> int:
     return _check(load().ragc_kv8_append(_ref(pool), _ref(batch), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
                                          q_heads, stream or None))
+
+
+def ragc_kv8_attn_workspace(pool: ragc_kv_pool, batch: ragc_batch, q_heads: int, flags: int = 0) -> int:
+    return _check(int(load().ragc_kv8_attn_workspace(_ref(pool), _ref(batch), q_heads, flags)))
+
+
+def ragc_kv8_attn(pool, batch, q, out, q_heads: int, softmax_scale: float, flags: int = 0, workspace=None, workspace_bytes: int = 0,
+                  stream: int = 0) -> int:
+    return _check(load().ragc_kv8_attn(_ref(pool), _ref(batch), _ptr(q), _ptr(out), q_heads, softmax_scale, flags, _ptr(workspace),
+                                       workspace_bytes, stream or None))
 
 
 def ragc_kv_swap(pool, host_k, host_v, host_block_stride_elems: int, num_host_slots: int, dev_block_ids: np.ndarray,

@@ -497,6 +497,75 @@ int run_f32(const ragc::AttnLaunch& a, const ragc_batch* batch, const HostMeta& 
                     [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_attn_f32(a, wk, entries, plan.rows, plan.waves, s); });
 }
 
+// How attention over an 8-bit pool runs a batch: rows per item and 16-key blocks per copy (0: items are not split).
+struct Kv8Plan {
+    std::vector<int32_t> order;
+    int rows = ragc::kKv8Rows;
+    int chunk = 0;
+    int64_t entries = 0, workspace = 0;
+};
+
+inline int64_t kv8_copies(const HostMeta& h, int r, int chunk) {
+    const int64_t blocks = ((int64_t)h.prefix_len[r] + h.new_len[r] + RAGC_BLOCK_SIZE - 1) / RAGC_BLOCK_SIZE;
+    return chunk == 0 ? 1 : (blocks + chunk - 1) / chunk;
+}
+
+int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& h, int group, uint32_t flags, Kv8Plan* plan) {
+    order_requests(h, batch->num_reqs, &plan->order);
+    int64_t max_rows = 0;
+    for (int r : plan->order) max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
+    plan->rows = max_rows <= ragc::kKv8Rows ? ragc::kKv8Rows : ragc::kKv8WideRows;
+    int64_t work = 0;  // blocks that workgroups walk
+    for (int r : plan->order) work += row_tiles(h, r, group, plan->rows) * kv8_copies(h, r, 1) * pool->kv_heads;
+    const int64_t cus = cu_count();
+    if (!(flags & RAGC_ATTN_NO_SPLIT)) {
+        const int64_t chunk = std::max<int64_t>(32, (work / (2 * cus) + 15) / 16 * 16);
+        if (chunk <= INT32_MAX / 2) plan->chunk = (int)chunk;
+    }
+    bool split = false;
+    for (int r : plan->order) {
+        const int64_t copies = kv8_copies(h, r, plan->chunk);
+        split |= copies > 1;
+        plan->entries += row_tiles(h, r, group, plan->rows) * copies;
+    }
+    if (!split) plan->chunk = 0;
+    if (plan->entries > INT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group of the batch too large");
+    if (split) plan->workspace = plan->entries * pool->kv_heads * ragc::attn_partial_bytes(pool->head_dim, plan->rows);
+    return RAGC_OK;
+}
+
+// Enqueues `launch(list, entries)` for all entries of a plan, as many per launch as the kernel arguments and a grid hold.
+template <class Launch>
+int run_kv8_list(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, const Launch& launch) {
+    // the merge has a workgroup per entry, kv head and row
+    const int64_t max_workgroups = std::min<int64_t>(ragc::kAttnMaxWorkgroups / ragc::kKv8WideRows, UINT32_MAX / a.head_div);
+    const int64_t per_launch = std::max<int64_t>(1, max_workgroups / a.kv_heads);
+    int64_t slots = 0;
+    for (size_t i = 0; i < plan.order.size(); i += ragc::kAttnMaxReqs) {
+        ragc::AttnWork wk;
+        wk.n_reqs = (int32_t)std::min<size_t>(ragc::kAttnMaxReqs, plan.order.size() - i);
+        wk.splits = plan.chunk;
+        wk.part_base = (int32_t)slots;
+        int64_t entries = 0;
+        for (int j = 0; j < wk.n_reqs; ++j) {
+            const int r = plan.order[i + j];
+            wk.first[j] = (int32_t)entries;
+            wk.req[j] = {h.prefix_len[r], h.new_len[r], h.new_start[r], r};
+            entries += row_tiles(h, r, a.group, plan.rows) * kv8_copies(h, r, plan.chunk);
+        }
+        for (int j = wk.n_reqs; j % ragc::kAttnReqStep; ++j) wk.first[j] = INT32_MAX;
+        for (int64_t e0 = 0; e0 < entries; e0 += per_launch) {
+            wk.entry0 = (int32_t)e0;
+            const hipError_t e = launch(wk, (int)std::min<int64_t>(per_launch, entries - e0));
+            if (e != hipSuccess) return fail(RAGC_ERR_HIP, "attention launch: %s (earlier launches of this call stay enqueued)", hipGetErrorString(e));
+        }
+        slots += entries;
+    }
+    return RAGC_OK;
+}
+
+constexpr uint32_t kKv8AttnFlags = RAGC_ATTN_NO_SPLIT | RAGC_ATTN_VALIDATE;
+
 // ---- partial results of key-split work items for callers that cannot allocate --------------
 // One array per GPU (every device that loads the library holds its own copy until the process
 // ends).  Host code must never pass the array's name to a kernel: that name is a host-side
@@ -523,6 +592,32 @@ int static_scratch(void** out) {
     }
     *out = g_scratch_ptr[dev];
     return RAGC_OK;
+}
+
+ragc::AttnLaunch make_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale) {
+    const auto magic = [](uint32_t d) { return d == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); };
+    ragc::AttnLaunch a;
+    a.pool_k = pool->k;
+    a.pool_v = pool->v;
+    a.block_stride = pool->block_stride_elems;
+    a.block_table = batch->block_table;
+    a.q = q;
+    a.k_new = nullptr;
+    a.v_new = nullptr;
+    a.out = out;
+    a.partial = nullptr;
+    a.table_stride = batch->table_stride;
+    a.kv_heads = pool->kv_heads;
+    a.head_dim = pool->head_dim;
+    a.q_heads = q_heads;
+    a.group = q_heads / pool->kv_heads;
+    a.group_magic = magic(a.group);
+    a.scale_log2e = softmax_scale * 1.44269504088896340736f;
+    a.fused_append = 0;
+    a.head_shift = pool->kv_heads % 8 == 0 ? 3 : 0;
+    a.head_div = (uint32_t)pool->kv_heads >> a.head_shift;
+    a.head_magic = magic(a.head_div);
+    return a;
 }
 
 int prefill_attn_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, const void* k_new,
@@ -552,28 +647,10 @@ int prefill_attn_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const v
     if (validate)
         if (int rc = validate_batch(pool, batch, h, (flags & RAGC_ATTN_APPEND_FUSED) != 0)) return rc;
 
-    const auto magic = [](uint32_t d) { return d == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); };
-    ragc::AttnLaunch a;
-    a.pool_k = pool->k;
-    a.pool_v = pool->v;
-    a.block_stride = pool->block_stride_elems;
-    a.block_table = batch->block_table;
-    a.q = q;
+    ragc::AttnLaunch a = make_attn(pool, batch, q, out, q_heads, softmax_scale);
     a.k_new = k_new;
     a.v_new = v_new;
-    a.out = out;
-    a.partial = nullptr;
-    a.table_stride = batch->table_stride;
-    a.kv_heads = pool->kv_heads;
-    a.head_dim = pool->head_dim;
-    a.q_heads = q_heads;
-    a.group = q_heads / pool->kv_heads;
-    a.group_magic = magic(a.group);
-    a.scale_log2e = softmax_scale * 1.44269504088896340736f;
     a.fused_append = (flags & RAGC_ATTN_APPEND_FUSED) ? 1 : 0;
-    a.head_shift = pool->kv_heads % 8 == 0 ? 3 : 0;
-    a.head_div = (uint32_t)pool->kv_heads >> a.head_shift;
-    a.head_magic = magic(a.head_div);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (pool->dtype == RAGC_DTYPE_F32) {
         return run_f32(a, batch, h, s);
@@ -758,6 +835,55 @@ int ragc_prefill_attn_static(const ragc_kv_pool* pool, const ragc_batch* batch, 
                              const void* v_new, void* out, int32_t q_heads, float softmax_scale, uint32_t flags,
                              void* stream) {
     return prefill_attn_impl(pool, batch, q, k_new, v_new, out, q_heads, softmax_scale, flags, nullptr, 0, true, stream);
+}
+
+int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) {
+    g_err[0] = 0;
+    if (int rc = check_pool(pool, 1)) return rc;
+    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+    BatchInfo info;
+    HostMeta h;
+    if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
+    if (batch->num_reqs == 0 || info.total_new == 0) return 0;
+    Kv8Plan plan;
+    if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
+    return plan.workspace;
+}
+
+int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
+                  uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    if (int rc = check_pool(pool, 1)) return rc;
+    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+    if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+        return fail(RAGC_ERR_SHAPE, "softmax_scale must be positive and finite");
+    const bool validate = (flags & RAGC_ATTN_VALIDATE) != 0;
+    BatchInfo info;
+    HostMeta h;
+    if (int rc = check_batch(pool, batch, true, validate, &h, &info)) return rc;
+    if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
+    if (!q || !out) return fail(RAGC_ERR_NULL, "q / out is NULL");
+    if (!aligned16(q) || !aligned16(out)) return fail(RAGC_ERR_ALIGN, "q / out must be 16-byte aligned");
+    if (validate)
+        if (int rc = validate_batch(pool, batch, h, false)) return rc;
+    ragc::AttnLaunch a = make_attn(pool, batch, q, out, q_heads, softmax_scale);
+    Kv8Plan plan;
+    if (int rc = plan_kv8(pool, batch, h, a.group, flags, &plan)) return rc;
+    if (plan.workspace > 0) {
+        if (!workspace || (int64_t)workspace_bytes < plan.workspace)
+            return fail(RAGC_ERR_WORKSPACE, "workspace of %lld bytes needed (ragc_kv8_attn_workspace), %zu given", (long long)plan.workspace, workspace_bytes);
+        if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(RAGC_ERR_ALIGN, "workspace must be 256-byte aligned");
+        a.partial = workspace;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    int rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_kv8_attn_rows(a, wk, entries, plan.rows, s); });
+    if (rc == RAGC_OK && plan.chunk > 0)
+        rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_kv8_merge(a, wk, entries, plan.rows, s); });
+    return rc;
 }
 
 int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new, void* stream) {

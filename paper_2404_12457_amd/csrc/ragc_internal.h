@@ -116,6 +116,13 @@ hipError_t launch_attn_bf16_rows(const AttnLaunch& a, const AttnWork& wk, int en
 // second pass after a launch of split items of `rows` rows: combines the partial results into `out`
 hipError_t launch_attn_bf16_merge(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s);
 
+// 8-bit cache (block_stride in bytes).  wk.splits is the number of 16-key blocks that one copy of an item takes (0: one copy takes
+// all); a request has as many copies per row tile as its length asks for, an entry each, and every entry has a slot in the workspace.
+constexpr int kKv8Rows = 16, kKv8WideRows = 32;  // rows per item
+hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s);
+// second pass: combines the copies' states of the requests that have more than one
+hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s);
+
 hipError_t launch_append(const PagedBatch& b, void* pool_k, void* pool_v, const void* k_new, const void* v_new,
                          int32_t total_new, int esize, hipStream_t s);
 

@@ -224,3 +224,195 @@ def test_append_rope_then_prefill_attention_is_attention_over_rotated_rows():
         k, v = (x[c.h_table[r, pos // 16], :, pos % 16] for x in tiles)
         want = OA.prefill_attn(c.host(c.q)[rows], k, v, p, 128**-0.5)
         assert np.max(np.abs(c.host(out)[rows] - want)) <= 2e-2
+
+
+# ---- attention ------------------------------------------------------------------------------
+# Against exact arithmetic on the same bytes.  Probabilities are rounded to bf16 (2^-9 relative each on average over many, 2^-8 at most)
+# and so is the output: |error| <= 2^-8 |out| + 2^-8 sum_j p_j |v_j|, plus the scores' own error in the exponent.  With e4m3 K and bf16 Q
+# as two e4m3 numbers the matrix unit keeps 16 bits below the largest product of a group of 16: at most 16 * 2^-16 of sum |q k| per
+# score, times scale, and twice that (numerator and denominator) of sum_j p_j |v_j|.
+def _attention(c, q, scale):
+    """(exact output, bound of the error), [rows, q_heads, head_dim]."""
+    want, tol = np.zeros((c.rows, c.hq, c.d)), np.zeros((c.rows, c.hq, c.d))
+    planes = [p.cpu().numpy() for p in c.planes]
+    for r, p, n, rows in c.spans():
+        k, v = (O.read_tokens(x, c.h_table[r], p + n, c.hkv, c.d, is_k) for x, is_k in zip(planes, (True, False)))
+        hidden = np.arange(p + n)[None] > p + np.arange(n)[:, None]
+        for h in range(c.hq):
+            g = h // (c.hq // c.hkv)
+            x = q[rows, h]
+            s = np.where(hidden, -np.inf, scale * (x @ k[:, g].T))
+            e = np.exp(s - s.max(-1, keepdims=True))
+            w = e / e.sum(-1, keepdims=True)
+            vv = np.where(np.isnan(v[:, g]), 0.0, v[:, g])
+            seen_nan = (~hidden).astype(float) @ np.isnan(v[:, g])
+            want[rows, h] = np.where(seen_nan > 0, np.nan, w @ vv)
+            off = scale * 2.0**-12 * np.where(hidden, 0.0, np.abs(x) @ np.abs(k[:, g]).T).max(-1, keepdims=True)
+            tol[rows, h] = 2.0**-8 * np.abs(want[rows, h]) + (2.0**-8 + 2 * off) * (w @ np.abs(vv)) + 1e-30
+    return want, tol
+
+
+def _run(c, scale, flags=0, q=None, out=None):
+    need = B.ragc_kv8_attn_workspace(c.pool, c.batch, c.hq, flags)
+    ws = torch.full((max(need, 1),), 255, dtype=torch.uint8, device="cuda")  # NaN everywhere: nothing may be read before it is written
+    out = torch.full_like(c.q, 7.0) if out is None else out
+    B.ragc_kv8_attn(c.pool, c.batch, c.q if q is None else q, out, c.hq, scale, flags, ws, need, _stream())
+    torch.cuda.synchronize()
+    return out
+
+
+def _check(c, scale, flags=0):
+    want, tol = _attention(c, c.host(c.q), scale)
+    out = _run(c, scale, flags)
+    got = c.host(out)[c.first:]
+    want, tol = want[c.first:], tol[c.first:]
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    worst = float(np.nanmax(np.abs(got - want) / tol)) if not np.isnan(want).all() else 0.0
+    assert worst <= 1
+    assert torch.all(out[:c.first] == 7)
+    again = _run(c, scale, flags)
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))  # the order of sums is fixed
+    return out
+
+
+ATTN = {
+    "steps": [(int(p), 1) for p in np.random.Generator(np.random.PCG64(2)).integers(0, 600, 70)],
+    "one": [(0, 1)],
+    "short": [(15, 1), (16, 1), (31, 1), (32, 1), (33, 1), (0, 2), (14, 3), (0, 0), (255, 1)],
+    "few": [(40, 4), (513, 3), (0, 7), (1000, 5)],
+    "questions": [(100, 33), (0, 40), (47, 17), (260, 1), (15, 64)],
+    "prompts": [(0, 300), (301, 129), (64, 64), (1000, 200), (3, 1)],
+    "long_step": [(9000, 1), (300, 1)],
+    "long_question": [(5000, 19)],
+}
+HEADS = [(8, 2, 128), (4, 4, 64), (7, 1, 128), (28, 4, 64), (16, 1, 128), (20, 1, 64), (3, 3, 128), (64, 8, 128)]
+
+
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("lens", list(ATTN))
+def test_kv8_attention(lens, hq, hkv, d):
+    c = Case(ATTN[lens], hq, hkv, d, seed=hq, pad=hkv % 3, first_row=hkv % 2)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    _check(c, d**-0.5)
+
+
+@pytest.mark.parametrize("lens", ["long_step", "long_question", "few"])
+def test_kv8_attention_without_a_split(lens):
+    c = Case(ATTN[lens], 8, 2, 128, seed=9)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    assert B.ragc_kv8_attn_workspace(c.pool, c.batch, 8, B.RAGC_ATTN_NO_SPLIT) == 0
+    _check(c, 128**-0.5, B.RAGC_ATTN_NO_SPLIT)
+
+
+@pytest.mark.parametrize("lens", ["steps", "few", "questions", "prompts", "long_step", "long_question"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_attention_with_a_sharp_softmax(lens, d):
+    """Scores of some tens: the running reference is raised often."""
+    c = Case(ATTN[lens], 8, 2, d, seed=10)
+    c.fill_prefixes()
+    c.q.mul_(6.0)
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    _check(c, d**-0.5)
+
+
+@pytest.mark.parametrize("lens", ["short", "few", "questions", "prompts", "long_step"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_attention_nan_goes_to_the_rows_that_see_it(lens, d):
+    """NaN in V of every request's fourth token from the end and in K of another's; slots behind the last token are NaN too."""
+    c = Case(ATTN[lens], 8, 2, d, seed=11)
+    c.fill_prefixes()
+    for r, (p, n) in enumerate(zip(c.h_prefix, c.h_new)):
+        at = int(c.h_start[r]) + int(n) - 4
+        if n >= 4:
+            c.v_new[at, 0, 5] = float("nan")
+            c.v_new[at + 2, 1] = float("nan")
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    planes = [p.cpu().numpy() for p in c.planes]
+    for plane, is_k in zip(planes, (True, False)):
+        order = O.byte_of(d, is_k)
+        for r, (p, n) in enumerate(zip(c.h_prefix, c.h_new)):
+            end = int(p) + int(n)
+            if end % 16:
+                for h in range(2):
+                    plane[c.h_table[r, end // 16], h * 16 * d + order[end % 16:]] = 0x7F
+    for plane, host in zip(c.planes, planes):
+        plane.copy_(torch.from_numpy(host))
+    _check(c, d**-0.5)
+
+
+def test_kv8_attention_nan_in_k_reaches_the_rows_that_see_the_key():
+    c = Case([(20, 50)], 4, 2, 128, seed=12)
+    c.fill_prefixes()
+    c.k_new[30, 1] = float("nan")
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    out = c.host(_run(c, 128**-0.5))
+    assert not np.isnan(out[:30]).any() and np.isnan(out[30:, 2:]).all() and not np.isnan(out[30:, :2]).any()
+
+
+@pytest.mark.parametrize("lens", ["few", "prompts"])
+def test_kv8_attention_scales_of_all_sizes(lens):
+    """Blocks of very different magnitude next to each other; q is small where K is large."""
+    c = Case(ATTN[lens], 4, 2, 64, seed=13)
+    sat = 2 * 16 * 64
+    for plane in c.planes:
+        plane[:, :sat] &= 0xF7  # no NaN codes
+    c.planes[0][:, sat:sat + 2] = torch.from_numpy(c.rng.integers(95, 160, (c.blocks, 2)).astype(np.uint8)).cuda()
+    c.planes[1][:, sat:sat + 2] = torch.from_numpy(c.rng.integers(60, 200, (c.blocks, 2)).astype(np.uint8)).cuda()
+    c.q.mul_(2.0**-38)
+    _check(c, 0.125)
+
+
+def test_kv8_append_then_attention_equals_one_prefill():
+    """The run of the two as a server uses them: a prompt at once, or its first part, then the rest token by token.  The scales of partly
+    filled blocks may come about differently, so the second way is compared with the oracle on its own bytes and with the first loosely."""
+    whole = Case([(0, 45)], 8, 2, 128, seed=14, room=16)
+    cs, keep, rope = _rope(whole, 128, False)
+    q0 = whole.q.clone()
+    q = torch.empty_like(q0)
+    B.ragc_kv8_append(whole.pool, whole.batch, rope, q0, whole.k_new, whole.v_new, q, 8, _stream())
+    whole.q.copy_(q)
+    once = _check(whole, 128**-0.5)
+    parts = Case([(0, 45)], 8, 2, 128, seed=14, room=16)
+    got = []
+    for lo, hi in [(0, 30)] + [(i, i + 1) for i in range(30, 45)]:
+        hp, hn, hs = (np.asarray(x, np.int32) for x in ([lo], [hi - lo], [0, hi - lo]))
+        dev = [torch.from_numpy(a).cuda() for a in (hp, hn, hs)]
+        batch = B.make_batch(1, parts.h_table.shape[1], *dev, parts.dev[3], hp, hn, hs, parts.h_table)
+        qq, out = torch.empty_like(q0[lo:hi]), torch.empty_like(q0[lo:hi])
+        B.ragc_kv8_append(parts.pool, batch, rope, q0[lo:hi], parts.k_new[lo:hi], parts.v_new[lo:hi], qq, 8, _stream())
+        assert torch.equal(qq, q[lo:hi])
+        B.ragc_kv8_attn(parts.pool, batch, qq, out, 8, 128**-0.5, 0, None, 0, _stream())
+        got.append(out)
+    got = torch.cat(got).double()
+    assert float((got - once.double()).norm() / once.double().norm()) < 2e-2
+
+
+def test_kv8_attention_on_streams_and_in_a_graph():
+    """Two batches on two streams with workspaces of their own, and a captured call replayed over changed bytes and tables."""
+    cases = [Case([(3000, 1), (70, 1)], 8, 2, 128, seed=15), Case([(2500, 2), (9, 1)], 8, 2, 64, seed=16)]
+    streams, outs, spaces = [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    for c in cases:
+        c.fill_prefixes()
+        B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+        spaces.append(torch.empty(max(1, B.ragc_kv8_attn_workspace(c.pool, c.batch, c.hq)), dtype=torch.uint8, device="cuda"))
+        outs.append(torch.empty_like(c.q))
+    want = [_run(c, 0.1) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s, o, w in zip(cases, streams, outs, spaces):
+            B.ragc_kv8_attn(c.pool, c.batch, c.q, o, c.hq, 0.1, 0, w, w.numel(), s.cuda_stream)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+    c, space = cases[0], spaces[0]
+    side, graph, out = torch.cuda.Stream(), torch.cuda.CUDAGraph(), torch.empty_like(c.q)
+    with torch.cuda.graph(graph, stream=side):
+        B.ragc_kv8_attn(c.pool, c.batch, c.q, out, c.hq, 0.1, 0, space, space.numel(), side.cuda_stream)
+    for _ in range(3):
+        c.q.normal_()
+        c.dev[3][0, :50] = c.dev[3][0, :50].flip(0)  # other blocks, as far as the replay is concerned
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, _run(c, 0.1))

@@ -178,3 +178,36 @@ def test_swap_of_8_bit_pools_counts_the_scales():
     assert _code(B.ragc_kv_swap, _pool8(), A, A, need - 16, 4, ids, ids, B.RAGC_SWAP_TO_HOST) == B.RAGC_ERR_SHAPE
     assert _code(B.ragc_kv_swap, _pool8(), A, A, need + 8, 4, ids, ids, B.RAGC_SWAP_TO_HOST) == B.RAGC_ERR_ALIGN
     assert B.ragc_kv_swap(_pool8(), A, A, need, 4, np.zeros(0, np.int32), np.zeros(0, np.int32), B.RAGC_SWAP_TO_HOST) == 0
+
+
+def _attn_code(pool=None, batch=None, q=A, o=A, hq=8, scale=0.1, flags=0, ws=None, n=0):
+    return _code(B.ragc_kv8_attn, pool or _pool8(), batch or _batch(), q, o, hq, scale, flags, ws, n)
+
+
+def test_kv8_attention_refuses():
+    for dtype in (B.RAGC_DTYPE_F32, B.RAGC_DTYPE_BF16, 5):
+        assert _attn_code(pool=_pool(dtype)) == B.RAGC_ERR_SHAPE
+        assert _code(B.ragc_kv8_attn_workspace, _pool(dtype), _batch(), 8) == B.RAGC_ERR_SHAPE
+    assert _attn_code(hq=3) == B.RAGC_ERR_SHAPE and _attn_code(hq=0) == B.RAGC_ERR_SHAPE
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert _attn_code(scale=scale) == B.RAGC_ERR_SHAPE
+    assert _attn_code(flags=B.RAGC_ATTN_APPEND_FUSED) == B.RAGC_ERR_SHAPE and _attn_code(flags=0x80) == B.RAGC_ERR_SHAPE
+    assert _code(B.ragc_kv8_attn_workspace, _pool8(), _batch(), 8, B.RAGC_ATTN_APPEND_FUSED) == B.RAGC_ERR_SHAPE
+    assert _attn_code(q=None) == B.RAGC_ERR_NULL and _attn_code(o=None) == B.RAGC_ERR_NULL
+    assert _attn_code(q=A + 8) == B.RAGC_ERR_ALIGN and _attn_code(o=A + 2) == B.RAGC_ERR_ALIGN
+    assert _attn_code(batch=_batch(dev=None)) == B.RAGC_ERR_NULL
+    assert _attn_code(batch=_batch(p=(60,), n=(10,))) == B.RAGC_ERR_RANGE
+    assert _attn_code(batch=_batch(p=(20,), n=(5,), table=np.array([[1, 64, 0, 0]], np.int32))) == B.RAGC_ERR_RANGE
+    assert B.ragc_kv8_attn(_pool8(), _batch(n=(0,)), None, None, 8, 0.1) == 0
+
+
+def test_kv8_attention_workspace():
+    long = _batch(p=(100000,), n=(1,), stride=6251)
+    need = B.ragc_kv8_attn_workspace(_pool8(num_blocks=7000), long, 8)
+    assert need > 0 and need % (2 * 16 * (128 + 2) * 4) == 0
+    assert B.ragc_kv8_attn_workspace(_pool8(num_blocks=7000), long, 8, B.RAGC_ATTN_NO_SPLIT) == 0
+    assert B.ragc_kv8_attn_workspace(_pool8(), _batch(), 8) == 0 and B.ragc_kv8_attn_workspace(_pool8(), _batch(n=(0,)), 8) == 0
+    p = _pool8(num_blocks=7000)
+    assert _attn_code(pool=p, batch=long) == B.RAGC_ERR_WORKSPACE
+    assert _attn_code(pool=p, batch=long, ws=A, n=need - 1) == B.RAGC_ERR_WORKSPACE
+    assert _attn_code(pool=p, batch=long, ws=A + 16, n=need) == B.RAGC_ERR_ALIGN
