@@ -20,7 +20,7 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libragc.so")
 CALIB_LIB = os.path.join(HERE, "libragc_calib.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))  # for this interpreter, host code only
-SOURCES = ["ragc_api.cpp", "ragc_ctl.cpp", "kv_ops.hip", "kv_rope.hip", "kv8_append.hip", "kv8_attn_rows.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_rows.hip"]
+SOURCES = ["ragc_api.cpp", "ragc_ctl.cpp", "kv_ops.hip", "kv_rope.hip", "kv8_append.hip", "kv8_attn.hip", "kv8_attn_rows.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_rows.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
     # packed fp32 math is kept off on this target (see the build notes)

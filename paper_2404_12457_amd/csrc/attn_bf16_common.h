@@ -20,6 +20,14 @@ constexpr float kRescaleThreshold = 8.f;  // log2 units
 constexpr float kRaiseSum = 256.f;        // of a lane's probabilities of a tile
 constexpr bf16x2 kOnes2 = {(__bf16)1.0f, (__bf16)1.0f};
 
+template <int N, class F>
+__device__ __forceinline__ void static_for(const F& f) {
+    if constexpr (N > 0) {
+        static_for<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
 // Wave-wide copy of 64 x 16 bytes from global memory straight into LDS: lane i's 16 bytes
 // land at lds_addr + 16*i.  Issued as inline assembly on purpose: the compiler's own
 // bookkeeping for this instruction drains every outstanding load before the next LDS read,
@@ -31,6 +39,11 @@ constexpr bf16x2 kOnes2 = {(__bf16)1.0f, (__bf16)1.0f};
 __device__ __forceinline__ void dma_16B_per_lane(const void* gptr, uint32_t lds_addr) {
     lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);  // wave-uniform by construction; make the register class explicit
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
+// The same for a dword per lane: lane i's lands at lds_addr + 4*i.
+__device__ __forceinline__ void dma_4B_per_lane(const void* gptr, uint32_t lds_addr) {
+    lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(gptr) : "memory", "m0");
 }
 // N runs of 64 x 16 bytes from a wave-uniform base address: run i comes from sbase + off[i] + OFF0 + 1024 i and lands at
 // lds_addr + OFF0 + 1024 i (the instruction's offset counts on both sides, so one write of M0 serves all).  sbase is in scalar

@@ -18,14 +18,13 @@
 // fourth chunk c from i / 16 on.  V codes turn around in LDS.  Which block: item j of the launch belongs to the largest request
 // r with (new_start[r] - new_start[0] + 30 r) / 16 <= j, which leaves every request room for as many blocks as n tokens can touch
 // from any offset, (n + 30) / 16, so no list has to be made on the host and a captured launch follows the device arrays.
+#include "kv8_codes.h"
 #include "kv_rope.h"
 
 namespace ragc {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-
-constexpr int kCodeNan = 0x7f;
 
 // |x| of a finite number as a whole number that keeps its order and whether it lies above a border of 20 bits
 __device__ __forceinline__ uint32_t size_key(double x) {
@@ -45,16 +44,6 @@ __device__ __forceinline__ float round_to_odd(double x) {
     uint32_t u = __float_as_uint(f);
     if (back != x) u = (__builtin_fabs(back) > __builtin_fabs(x) ? u - 1 : u) | 1;
     return __uint_as_float(u);
-}
-// four numbers of at most 448, or not finite, to codes
-__device__ __forceinline__ uint32_t encode4(const float* x) {
-    int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], v, true);
-    uint32_t u = (uint32_t)v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(__builtin_fabsf(x[i]) <= 448.f)) u = (u & ~(0xffu << 8 * i)) | (uint32_t)kCodeNan << 8 * i;
-    return u;
 }
 // codes of a scale 2^by times the new one, rounded to that
 __device__ __forceinline__ uint32_t raise4(uint32_t codes, int by) {

@@ -3,6 +3,7 @@
 #pragma once
 #include "attn_bf16_common.h"
 #include "attn_work.h"
+#include "kv8_codes.h"
 
 namespace ragc {
 namespace {
@@ -20,8 +21,9 @@ __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((ui
 
 // 0x80 in every byte that is a NaN code
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) { return ((codes & kNoNan) + 0x01010101u) & 0x80808080u; }
-// the codes with NaN made 0, and 1.0 (0x38) where there was one and 0 elsewhere
-__device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~((nan_bytes(codes) >> 7) * 0xffu); }
+// the codes with NaN made 0, but for the bytes of `except`
+__device__ __forceinline__ uint32_t without_nan(uint32_t codes, uint32_t except = 0) { return codes & (except | ~((nan_bytes(codes) >> 7) * 0xffu)); }
+// 1.0 (0x38) where there is a NaN and 0 elsewhere
 __device__ __forceinline__ uint32_t where_nan(uint32_t codes) { return (nan_bytes(codes) >> 7) * 0x38u; }
 // bytes of the four keys from `key` on that lie below `limit`
 __device__ __forceinline__ uint32_t below(int key, int limit) {

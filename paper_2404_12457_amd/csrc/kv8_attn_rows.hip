@@ -371,8 +371,10 @@ void merge_one(const AttnLaunch& a, const Work& wk, int entries, hipStream_t s) 
 }
 template <class Work>
 void merge_list(const AttnLaunch& a, const Work& wk, int entries, int rows, hipStream_t s) {
-    if (a.head_dim == 64) rows == 16 ? merge_one<64, 16>(a, wk, entries, s) : merge_one<64, 32>(a, wk, entries, s);
-    else rows == 16 ? merge_one<128, 16>(a, wk, entries, s) : merge_one<128, 32>(a, wk, entries, s);
+    const bool d64 = a.head_dim == 64;
+    if (rows == kKv8Rows) d64 ? merge_one<64, kKv8Rows>(a, wk, entries, s) : merge_one<128, kKv8Rows>(a, wk, entries, s);
+    else if (rows == kKv8WideRows) d64 ? merge_one<64, kKv8WideRows>(a, wk, entries, s) : merge_one<128, kKv8WideRows>(a, wk, entries, s);
+    else d64 ? merge_one<64, kKv8TallRows>(a, wk, entries, s) : merge_one<128, kKv8TallRows>(a, wk, entries, s);
 }
 
 }  // namespace

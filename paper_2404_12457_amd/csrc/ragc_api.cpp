@@ -501,6 +501,7 @@ int run_f32(const ragc::AttnLaunch& a, const ragc_batch* batch, const HostMeta& 
 struct Kv8Plan {
     std::vector<int32_t> order;
     int rows = ragc::kKv8Rows;
+    int groups = 1;  // of items of kKv8TallRows rows
     int chunk = 0;
     int64_t entries = 0, workspace = 0;
 };
@@ -514,12 +515,17 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
     order_requests(h, batch->num_reqs, &plan->order);
     int64_t max_rows = 0;
     for (int r : plan->order) max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
-    plan->rows = max_rows <= ragc::kKv8Rows ? ragc::kKv8Rows : ragc::kKv8WideRows;
-    int64_t work = 0;  // blocks that workgroups walk
-    for (int r : plan->order) work += row_tiles(h, r, group, plan->rows) * kv8_copies(h, r, 1) * pool->kv_heads;
+    plan->rows = max_rows <= ragc::kKv8Rows ? ragc::kKv8Rows : max_rows <= ragc::kKv8WideRows ? ragc::kKv8WideRows : ragc::kKv8TallRows;
+    int64_t work = 0, items = 0;  // work: blocks that workgroups walk
+    for (int r : plan->order) {
+        const int64_t tiles = row_tiles(h, r, group, plan->rows) * pool->kv_heads;
+        items += tiles;
+        work += tiles * kv8_copies(h, r, 1);
+    }
     const int64_t cus = cu_count();
-    if (!(flags & RAGC_ATTN_NO_SPLIT)) {
-        const int64_t chunk = std::max<int64_t>(32, (work / (2 * cus) + 15) / 16 * 16);
+    const bool tall = plan->rows == ragc::kKv8TallRows;
+    if (!(flags & RAGC_ATTN_NO_SPLIT) && (!tall || items < cus)) {
+        const int64_t chunk = std::max<int64_t>(tall ? 64 : 32, (work / ((tall ? 1 : 2) * cus) + 15) / 16 * 16);
         if (chunk <= INT32_MAX / 2) plan->chunk = (int)chunk;
     }
     bool split = false;
@@ -529,6 +535,7 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
         plan->entries += row_tiles(h, r, group, plan->rows) * copies;
     }
     if (!split) plan->chunk = 0;
+    plan->groups = plan->entries * pool->kv_heads >= 2 * cus ? 1 : 2;
     if (plan->entries > INT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group of the batch too large");
     if (split) plan->workspace = plan->entries * pool->kv_heads * ragc::attn_partial_bytes(pool->head_dim, plan->rows);
     return RAGC_OK;
@@ -538,7 +545,7 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
 template <class Launch>
 int run_kv8_list(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, const Launch& launch) {
     // the merge has a workgroup per entry, kv head and row
-    const int64_t max_workgroups = std::min<int64_t>(ragc::kAttnMaxWorkgroups / ragc::kKv8WideRows, UINT32_MAX / a.head_div);
+    const int64_t max_workgroups = std::min<int64_t>(ragc::kAttnMaxWorkgroups / ragc::kKv8TallRows, UINT32_MAX / a.head_div);
     const int64_t per_launch = std::max<int64_t>(1, max_workgroups / a.kv_heads);
     int64_t slots = 0;
     for (size_t i = 0; i < plan.order.size(); i += ragc::kAttnMaxReqs) {
@@ -880,7 +887,9 @@ int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void*
         a.partial = workspace;
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    int rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_kv8_attn_rows(a, wk, entries, plan.rows, s); });
+    int rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) {
+        return plan.rows == ragc::kKv8TallRows ? ragc::launch_kv8_attn(a, wk, entries, plan.groups, s) : ragc::launch_kv8_attn_rows(a, wk, entries, plan.rows, s);
+    });
     if (rc == RAGC_OK && plan.chunk > 0)
         rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_kv8_merge(a, wk, entries, plan.rows, s); });
     return rc;

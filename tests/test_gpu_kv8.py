@@ -282,6 +282,7 @@ ATTN = {
     "few": [(40, 4), (513, 3), (0, 7), (1000, 5)],
     "questions": [(100, 33), (0, 40), (47, 17), (260, 1), (15, 64)],
     "prompts": [(0, 300), (301, 129), (64, 64), (1000, 200), (3, 1)],
+    "crowd": [(int(p), 17 + int(p) % 23) for p in np.random.Generator(np.random.PCG64(3)).integers(0, 300, 40)],
     "long_step": [(9000, 1), (300, 1)],
     "long_question": [(5000, 19)],
 }
