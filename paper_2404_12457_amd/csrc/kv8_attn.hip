@@ -145,17 +145,21 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         else dma_16B_per_lane(reinterpret_cast<const char*>(src) + lane * 16, dst);
     };
     auto window = [&](int step) { return (step >> 4 & 1) * 64 + 4 * (step & 15); };
-    // asks for V of a step, two steps ahead of its products, and notes where its K is
+    // where a step's block of V is; notes where its K is
     uint64_t k_src = 0;
-    auto fetch = [&](int step) {
+    auto locate = [&](int step) {
         const int id = __builtin_amdgcn_readfirstlane((int)win[window(step) + wq]);
         const long long at = (long long)id * a.block_stride + (long long)g * TILE;
         k_src = uniform_u64(pool_k + at);
-        copy_tile(uniform_u64(pool_v + at), lds_addr(raw_v));
-        // the next window: ids half way through this one, scales when those are there
-        if ((step & 15) == 4) dma_4B_per_lane(table + block_of((step | 15) + 1), lds_addr(win + ((step >> 4 & 1) ^ 1) * 64));
-        if ((step & 15) == 8) {
-            const int to = ((step >> 4 & 1) ^ 1) * 64;
+        return uniform_u64(pool_v + at);
+    };
+    // V of a step, two steps ahead of its products
+    auto fetch = [&](int step) { copy_tile(locate(step), lds_addr(raw_v)); };
+    // the next window: ids early in this one, scales when those are there
+    auto next_window = [&](int step) {
+        const int to = ((step >> 4 & 1) ^ 1) * 64;
+        if ((step & 15) == 2) dma_4B_per_lane(table + block_of((step | 15) + 1), lds_addr(win + to));
+        if ((step & 15) == 6) {
             const long long scales = (long long)(int)win[to + lane] * a.block_stride + scales_at;
             dma_4B_per_lane(pool_k + scales, lds_addr(win + 128 + to));
             dma_4B_per_lane(pool_v + scales, lds_addr(win + 256 + to));
@@ -172,6 +176,8 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
 #pragma unroll
         for (int x = 0; x < NC; ++x) vreg[x] = *reinterpret_cast<const lds_u32x4*>(v_from + x * 1024);
         v_scale = scale_of(win[256 + window(step) + wq] >> scale_shift & 255);
+    };
+    auto check_raw = [&](int step) {
         const int key = (t_lo + step * NG + grp) * 64 + wq * kBlock;
         if (key + kBlock > vis_min) {
             // The frontier: slots behind the last visible key may hold anything and become 0.  NaN in a key that some rows see and
@@ -189,12 +195,12 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
             if (nan != 0) nan_seen = 1;
         }
     };
-    auto store_v = [&](int slot, auto c_c) {  // one of the NC pieces
+    auto store_v = [&](int tile, auto c_c) {  // one of the NC pieces; tile: byte offset of the V tile
         constexpr int C = decltype(c_c)::value;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int dt = C * 4 + e;  // elements 16 dt + lane % 16: row (dt / DB) * 16 + lane % 16 of column tile dt % DB
-            *reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(v_dst + slot * VB + (dt % DB) * 1024 + (dt / DB) * 256) = widen4(vreg[C][e], v_scale);
+            *reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(v_dst + tile + (dt % DB) * 1024 + (dt / DB) * 256) = widen4(vreg[C][e], v_scale);
         }
     };
 
@@ -205,58 +211,59 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
     const float c = a.scale_log2e;
     const int k_lane = (l32 >> 4) * TILE + (l32 & 15) * 16 + kg * 512;
 
-    auto do_step = [&](int step, auto slot_c) {
-        constexpr int SLOT = decltype(slot_c)::value;
+    // One step.  FAST: two more steps follow, every key of this tile and of the next is visible to every row, the wave has rows: no branch
+    // stands between the products and what is brought under them (the compiler would move products behind it).
+    auto do_step = [&](int step, auto fast_c) {
+        constexpr bool FAST = decltype(fast_c)::value;
+        const int k_now = (step & 1) * KB, k_next = KB - k_now, v_now = (step & 1) * VB, v_next = VB - v_now;
         wait_vmcnt<0>();  // K of this step, V of the next and what windows were asked for have arrived
         block_barrier();  // every wave's part is in LDS, and every wave is done with the previous step
-        const bool more = step + 1 < nsteps, more2 = step + 2 < nsteps;
-        // part I of what the step brings for the next ones
-        auto bring = [&](auto i_c) {
-            constexpr int I = decltype(i_c)::value;
-            if (!more) return;
-            if (I == 0) {
-                copy_tile(k_src, k_dst + (SLOT ^ 1) * KB);
-                read_raw(step + 1);
-                if (more2) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read: its buffer is free
-                    fetch(step + 2);
-                }
-            }
-            store_v(SLOT ^ 1, i_c);
-        };
+        next_window(step);
+        const bool more = FAST || step + 1 < nsteps;
         const int tg = t_lo + step * NG + grp, key0 = tg * 64;
-        if (!wave_active || tg >= t_hi || key0 >= wave_vis_max) {
-            static_for<NC>(bring);
-            return;
+        if (!FAST) {
+            // what the next steps need, before the products: there are one or two such steps in an item
+            if (more) {
+                copy_tile(k_src, k_dst + k_next);
+                read_raw(step + 1);
+                check_raw(step + 1);
+                static_for<NC>([&](auto c_c) { store_v(v_next, c_c); });
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read: its buffer is free
+                if (step + 2 < nsteps) fetch(step + 2);
+            }
+            if (!wave_active || tg >= t_hi || key0 >= wave_vis_max) return;
         }
-        lds_char* const kst = lds0 + SLOT * KB + k_lane;
-        lds_char* const vst = lds_v + SLOT * VB + lane * 16;
-        // S^T = K Q^T; operands are read a step of the contraction ahead, and what the next steps need is brought under the products
+        lds_char* const kst = lds0 + k_now + k_lane;
+        lds_char* const vst = lds_v + v_now + lane * 16;
+        // S^T = K Q^T; operands are read a step of the contraction ahead
         f32x16 sacc[2] = {f32x16(0.f), f32x16(0.f)};
         i32x8 kbuf[NC][2];
         auto read_k = [&](int s) {
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
-                const u32x4 k0 = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(kst + sub * 2 * TILE + s * 1024);
-                const u32x4 k1 = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(kst + sub * 2 * TILE + s * 1024 + 256);
+                const u32x4 k0 = *reinterpret_cast<const lds_u32x4*>(kst + sub * 2 * TILE + s * 1024);
+                const u32x4 k1 = *reinterpret_cast<const lds_u32x4*>(kst + sub * 2 * TILE + s * 1024 + 256);
                 kbuf[s][sub] = i32x8{(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
             }
         };
-        read_k(0);
         int k_scale[2];
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) k_scale[sub] = (int)(win[128 + window(step) + 2 * sub + (l32 >> 4)] >> scale_shift);  // byte 0 counts
+        read_k(0);
+        if constexpr (FAST) read_raw(step + 1);
         static_for<NC>([&](auto s_c) {
             constexpr int S = decltype(s_c)::value;
-            if constexpr (S + 1 < NC) read_k(S + 1);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (S + 1 < NC) read_k(S + 1);
+            if constexpr (FAST && S == 0) copy_tile(k_src, k_dst + k_next);
             sacc[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kbuf[S][0], qhi[S], sacc[0], 0, 0, 0, k_scale[0], 0, q_scale);
             sacc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kbuf[S][1], qhi[S], sacc[1], 0, 0, 0, k_scale[1], 0, q_scale);
-            bring(s_c);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FAST) store_v(v_next, s_c);
             sacc[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kbuf[S][0], qlo[S], sacc[0], 0, 0, 0, k_scale[0], 0, q_scale_lo);
             sacc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kbuf[S][1], qlo[S], sacc[1], 0, 0, 0, k_scale[1], 0, q_scale_lo);
         });
+        __builtin_amdgcn_sched_barrier(0);
         // V operands two groups ahead, the first ones under the softmax
         constexpr int VGROUPS = 4 * DB / 2;
         bf16x8 vbuf[3][2];
@@ -268,14 +275,17 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         };
         read_v(std::integral_constant<int, 0>{});
         read_v(std::integral_constant<int, 1>{});
-        const bool frontier = key0 + 64 > wave_vis_min;
-        auto key_of = [&](int sub, int i) { return key0 + sub * 32 + (i >> 2) * 8 + kg * 4 + (i & 3); };
-        if (frontier) {
+        if constexpr (FAST) {
+#pragma unroll
+            for (int x = 0; x < NC; ++x) asm volatile("" ::"v"(vreg[x]));  // V has been read: its buffer is free
+            fetch(step + 2);
+        }
+        if (!FAST && key0 + 64 > wave_vis_min) {
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key_of(sub, i) >= my_vis) sacc[sub][i] = -INFINITY;
+                    if (key0 + sub * 32 + (i >> 2) * 8 + kg * 4 + (i & 3) >= my_vis) sacc[sub][i] = -INFINITY;
         }
         bf16x8 pb[4];
         float psum;
@@ -333,13 +343,16 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         copy_tile(k_src, k_dst);
         wait_vmcnt<0>();
         read_raw(0);
+        check_raw(0);
+        static_for<NC>([&](auto c_c) { store_v(0, c_c); });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (nsteps > 1) fetch(1);
-        static_for<NC>([&](auto c_c) { store_v(0, c_c); });
-        for (int step = 0; step < nsteps; step += 2) {
-            do_step(step, std::integral_constant<int, 0>{});
-            if (step + 1 < nsteps) do_step(step + 1, std::integral_constant<int, 1>{});
-        }
+        // steps whose tile and the next lie below vis_min, with two more behind them
+        const int clear = vis_min / 64 - t_lo - grp;  // tiles of this group from t_lo + grp on, in tiles
+        const int fast = wave_active ? max(0, min(nsteps - 2, clear <= 0 ? 0 : (clear + NG - 1) / NG - 1)) : 0;
+        int step = 0;
+        for (; step < fast; ++step) do_step(step, std::true_type{});
+        for (; step < nsteps; ++step) do_step(step, std::false_type{});
     }
 
     // ---- merge the wave groups through LDS (nothing is under way to it any more)
