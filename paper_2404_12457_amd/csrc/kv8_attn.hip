@@ -251,6 +251,7 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         for (int sub = 0; sub < 2; ++sub) k_scale[sub] = (int)(win[128 + window(step) + 2 * sub + (l32 >> 4)] >> scale_shift);  // byte 0 counts
         read_k(0);
         if constexpr (FAST) read_raw(step + 1);
+        __builtin_amdgcn_s_setprio(1);
         static_for<NC>([&](auto s_c) {
             constexpr int S = decltype(s_c)::value;
             __builtin_amdgcn_sched_barrier(0);
@@ -264,6 +265,7 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
             sacc[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kbuf[S][1], qlo[S], sacc[1], 0, 0, 0, k_scale[1], 0, q_scale_lo);
         });
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         // V operands two groups ahead, the first ones under the softmax
         constexpr int VGROUPS = 4 * DB / 2;
         bf16x8 vbuf[3][2];
@@ -325,6 +327,8 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
             weigh(m_run == -INFINITY ? 0.f : m_run);  // still no visible key: exp2(-inf - 0) = 0
         }
         l_run += psum;
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
         static_for<VGROUPS>([&](auto g_c) {
             constexpr int GI = decltype(g_c)::value;
             __builtin_amdgcn_sched_barrier(0);
@@ -335,6 +339,8 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
                 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vbuf[GI % 3][x], pb[2 * GI / DB], o, 0, 0, 0);
             }
         });
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
     };
 
     if (nsteps > 0) {
