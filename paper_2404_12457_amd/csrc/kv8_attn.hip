@@ -92,50 +92,20 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
     auto block_of = [&](int step) { return min((t_lo + min(step + (lane >> 2), max(nsteps - 1, 0)) * NG + grp) * 4 + (lane & 3), nblk - 1); };
     const int first_id = table[block_of(0)];
 
-    // ---- Q: hi and lo parts, elements 64 s + 32 kg .. + 31 of the row
-    i32x8 qhi[NC], qlo[NC];
-    int q_scale, q_scale_lo;  // e + 127 and that of the lo part
+    // ---- Q, elements 64 s + 32 kg .. + 31 of the row, under way with the first block ids
+    bf16x8 qv[NC][4];
     {
         const __bf16* const qp = static_cast<const __bf16*>(a.q) + ((long long)(s0 + my_tok) * Hq + g * G + (my_row - my_tok * G)) * D + kg * 32;
-        bf16x8 qv[NC][4];
-        uint32_t top = 0;
 #pragma unroll
         for (int s = 0; s < NC; ++s)
 #pragma unroll
             for (int x = 0; x < 4; ++x) qv[s][x] = *reinterpret_cast<const bf16x8*>(qp + s * 64 + x * 8);
-        const long long at = (long long)first_id * a.block_stride + scales_at;
-        win[lane] = (uint32_t)first_id;
-        win[128 + lane] = *reinterpret_cast<const uint32_t*>(pool_k + at);
-        win[256 + lane] = *reinterpret_cast<const uint32_t*>(pool_v + at);
-        if (tid == 0) nan_seen = 0;
-#pragma unroll
-        for (int s = 0; s < NC; ++s)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t u = __float_as_uint((float)qv[s][x][e]) & 0x7fffffffu;
-                    top = max(top, u < 0x7f800000u ? u : 0u);
-                }
-        top = max(top, __float_as_uint(other_half(__uint_as_float(top))));
-        // 448 = 1.75 * 2^8; a row of numbers below 2^-118 is far from mattering to any score
-        q_scale = max(5, (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u));
-        q_scale_lo = q_scale - 4;
-#pragma unroll
-        for (int s = 0; s < NC; ++s)
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                float f[4], r[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = __builtin_ldexpf((float)qv[s][x >> 1][(x & 1) * 4 + e], 127 - q_scale);
-                const uint32_t hi = encode4(f);
-                const bf16x4 back = widen4(hi, 1.f);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = (f[e] - (float)back[e]) * 16.f;  // at most half a step of hi, 16, times 16
-                qhi[s][x] = (int)hi;
-                qlo[s][x] = (int)encode4(r);
-            }
     }
+    asm volatile("" ::"v"(first_id));
+#pragma unroll
+    for (int s = 0; s < NC; ++s)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) asm volatile("" ::"v"(qv[s][x]));  // here before the first copies, which nothing then waits for but the first step
 
     // ---- what a wave brings: block wq of a tile
     const uint32_t k_dst = lds_addr(lds0) + wq * TILE;
@@ -145,16 +115,14 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         else dma_16B_per_lane(reinterpret_cast<const char*>(src) + lane * 16, dst);
     };
     auto window = [&](int step) { return (step >> 4 & 1) * 64 + 4 * (step & 15); };
-    // where a step's block of V is; notes where its K is
+    // V of a step's block, two steps ahead of its products; notes where its K is
     uint64_t k_src = 0;
-    auto locate = [&](int step) {
-        const int id = __builtin_amdgcn_readfirstlane((int)win[window(step) + wq]);
+    auto fetch = [&](int id) {
         const long long at = (long long)id * a.block_stride + (long long)g * TILE;
         k_src = uniform_u64(pool_k + at);
-        return uniform_u64(pool_v + at);
+        copy_tile(uniform_u64(pool_v + at), lds_addr(raw_v));
     };
-    // V of a step, two steps ahead of its products
-    auto fetch = [&](int step) { copy_tile(locate(step), lds_addr(raw_v)); };
+    auto id_of = [&](int step) { return __builtin_amdgcn_readfirstlane((int)win[window(step) + wq]); };
     // the next window: ids early in this one, scales when those are there
     auto next_window = [&](int step) {
         const int to = ((step >> 4 & 1) ^ 1) * 64;
@@ -204,6 +172,54 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         }
     };
 
+    // ---- the first tile, and under it the parts of Q
+    int q_scale, q_scale_lo;  // e + 127 and that of the lo part
+    i32x8 qhi[NC], qlo[NC];
+    {
+        const long long at = (long long)first_id * a.block_stride + scales_at;
+        const uint32_t ks = *reinterpret_cast<const uint32_t*>(pool_k + at), vs = *reinterpret_cast<const uint32_t*>(pool_v + at);
+        win[lane] = (uint32_t)first_id;
+        if (tid == 0) nan_seen = 0;
+        if (nsteps > 0) {
+            fetch(__builtin_amdgcn_readlane(first_id, wq));
+            copy_tile(k_src, k_dst);
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t u = __float_as_uint((float)qv[s][x][e]) & 0x7fffffffu;
+                    top = max(top, u);
+                }
+        top = max(top, __float_as_uint(other_half(__uint_as_float(top))));
+        const bool bad = top >= 0x7f800000u;
+        // 448 = 1.75 * 2^8; a row of numbers below 2^-118 is far from mattering to any score
+        q_scale = max(5, (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u));
+        q_scale_lo = q_scale - 4;
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                float f[4], r[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = __builtin_ldexpf((float)qv[s][x >> 1][(x & 1) * 4 + e], 127 - q_scale);
+                int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
+                const bf16x4 back = widen4((uint32_t)hi, 1.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = (f[e] - (float)back[e]) * 16.f;  // at most half a step of hi, 16, times 16
+                int lo = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], lo, true);
+                qhi[s][x] = bad ? (int)kNoNan : hi;  // a row with a number that is not finite is NaN: 0x7f four times
+                qlo[s][x] = bad ? 0 : lo;
+            }
+        win[128 + lane] = ks;
+        win[256 + lane] = vs;
+    }
+
     f32x16 oacc[DB];
 #pragma unroll
     for (int t = 0; t < DB; ++t) oacc[t] = f32x16(0.f);
@@ -229,7 +245,7 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
                 check_raw(step + 1);
                 static_for<NC>([&](auto c_c) { store_v(v_next, c_c); });
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read: its buffer is free
-                if (step + 2 < nsteps) fetch(step + 2);
+                if (step + 2 < nsteps) fetch(id_of(step + 2));
             }
             if (!wave_active || tg >= t_hi || key0 >= wave_vis_max) return;
         }
@@ -280,7 +296,7 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         if constexpr (FAST) {
 #pragma unroll
             for (int x = 0; x < NC; ++x) asm volatile("" ::"v"(vreg[x]));  // V has been read: its buffer is free
-            fetch(step + 2);
+            fetch(id_of(step + 2));
         }
         if (!FAST && key0 + 64 > wave_vis_min) {
 #pragma unroll
@@ -344,15 +360,13 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
     };
 
     if (nsteps > 0) {
-        block_barrier();  // nan_seen is 0, and the first window is in LDS
-        fetch(0);
-        copy_tile(k_src, k_dst);
         wait_vmcnt<0>();
         read_raw(0);
+        block_barrier();  // nan_seen is 0
         check_raw(0);
         static_for<NC>([&](auto c_c) { store_v(0, c_c); });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (nsteps > 1) fetch(1);
+        if (nsteps > 1) fetch(__builtin_amdgcn_readlane(first_id, 4 + wq));
         // steps whose tile and the next lie below vis_min, with two more behind them
         const int clear = vis_min / 64 - t_lo - grp;  // tiles of this group from t_lo + grp on, in tiles
         const int fast = wave_active ? max(0, min(nsteps - 2, clear <= 0 ? 0 : (clear + NG - 1) / NG - 1)) : 0;
@@ -464,16 +478,16 @@ void launch_one(const AttnLaunch& a, const Work& wk, int entries, hipStream_t s)
     hipLaunchKernelGGL((kv8_attn_kernel<D, NG, Work>), dim3((unsigned)entries * a.kv_heads), dim3(256 * NG), 0, s, a, wk);
 }
 template <class Work>
-void launch_list(const AttnLaunch& a, const Work& wk, int entries, int groups, hipStream_t s) {
-    if (a.head_dim == 64) groups == 2 ? launch_one<64, 2>(a, wk, entries, s) : launch_one<64, 1>(a, wk, entries, s);
-    else groups == 2 ? launch_one<128, 2>(a, wk, entries, s) : launch_one<128, 1>(a, wk, entries, s);
+void launch_list(const AttnLaunch& a, const Work& wk, int entries, int waves, hipStream_t s) {
+    if (a.head_dim == 64) waves == 8 ? launch_one<64, 2>(a, wk, entries, s) : launch_one<64, 1>(a, wk, entries, s);
+    else waves == 8 ? launch_one<128, 2>(a, wk, entries, s) : launch_one<128, 1>(a, wk, entries, s);
 }
 
 }  // namespace
 
-hipError_t launch_kv8_attn(const AttnLaunch& a, const AttnWork& wk, int entries, int groups, hipStream_t s) {
+hipError_t launch_kv8_attn(const AttnLaunch& a, const AttnWork& wk, int entries, int waves, hipStream_t s) {
     if (entries <= 0) return hipSuccess;
-    wk.n_reqs <= kAttnReqStep ? launch_list(a, short_list(wk), entries, groups, s) : launch_list(a, wk, entries, groups, s);
+    wk.n_reqs <= kAttnReqStep ? launch_list(a, short_list(wk), entries, waves, s) : launch_list(a, wk, entries, waves, s);
     return hipGetLastError();
 }
 

@@ -298,25 +298,28 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_rows_kernel(AttnLaunch a,
     }
 }
 
-// Combines the copies' states of every row of the requests that have more than one: out = sum_c O_c 2^(m_c - m) /
-// sum_c l_c 2^(m_c - m), m = max_c m_c.  One workgroup per (tile, kv head, row): 4 columns and every `groups`-th copy per thread.
-template <int D, int TR, class Work>
-__global__ __launch_bounds__(256) void kv8_merge_kernel(AttnLaunch a, Work wk) {
-    constexpr int TPR = D / 4, GROUPS = 256 / TPR;
-    __shared__ f32x4 os[GROUPS][TPR];
-    __shared__ float2 mls[GROUPS];
+// Combines the copies' states of every row: out = sum_c O_c 2^(m_c - m) / sum_c l_c 2^(m_c - m), m = max_c m_c.  The list holds the
+// requests that have more than one copy, an item per row tile, and in place of a request's number the slot of its first
+// entry.  A thread has four columns of a row and every SHARE-th copy; a workgroup 256 / SHARE of these, of the rows of one (tile, kv
+// head).  Few rows have many copies (decode steps), where many rows share the work there are few.
+template <int D, int TR, int SHARE, class Work>
+__global__ __launch_bounds__(256) void kv8_merge_kernel(AttnLaunch a, Work wk, int row_groups) {
+    constexpr int TPR = D / 4, RPW = 256 / (TPR * SHARE);
+    __shared__ f32x4 os[SHARE][RPW][TPR];
+    __shared__ float2 mls[SHARE][RPW];
     const int Hkv = a.kv_heads;
-    const int r = blockIdx.x % TR, g = blockIdx.x / TR % Hkv, entry = blockIdx.x / (TR * Hkv) + wk.entry0;
-    const WorkItem it = find_item(wk, entry, a.group, TR);
+    const int item = blockIdx.x / (row_groups * Hkv), g = blockIdx.x / row_groups % Hkv;
+    const WorkItem it = find_item(wk, item, a.group, TR);
     const int G = a.group, rows_total = it.new_len * G, tiles = (rows_total + TR - 1) / TR;
-    const int copies = copies_of(it.prefix + it.new_len, wk.splits), local = tiles - 1 - it.tile;
-    if (copies == 1 || local % copies != 0) return;
-    const int row = (tiles - 1 - local / copies) * TR + r;
-    if (row >= rows_total) return;
+    const int copies = copies_of(it.prefix + it.new_len, wk.splits);
+    // entries go from the last tile down, a tile's copies in a row
+    const int slot = it.req + (tiles - 1 - it.tile) * copies;
+    const int grp = threadIdx.x / (TPR * RPW), rr = threadIdx.x / TPR % RPW, d4 = threadIdx.x % TPR;
+    const int r = blockIdx.x % row_groups * RPW + rr, row = it.tile * TR + r;
+    if (row - rr >= rows_total) return;
     constexpr int PART = TR * (D + 2);
-    const float* const part0 = static_cast<const float*>(a.partial) + ((long long)(wk.part_base + entry) * Hkv + g) * PART;
+    const float* const part0 = static_cast<const float*>(a.partial) + ((long long)slot * Hkv + g) * PART;
     const long long copy_stride = (long long)Hkv * PART;
-    const int grp = threadIdx.x / TPR, d4 = threadIdx.x % TPR;
     float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float m1, float l1, f32x4 o1) {
@@ -328,25 +331,30 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(AttnLaunch a, Work wk) {
         m = top;
     };
     constexpr int AHEAD = 4;
-    for (int c0 = grp; c0 < copies; c0 += GROUPS * AHEAD) {
-        float2 ml[AHEAD];
-        f32x4 oc[AHEAD];
+    if (row < rows_total) {  // rows behind the last were not written
+        for (int c0 = grp; c0 < copies; c0 += SHARE * AHEAD) {
+            float2 ml[AHEAD];
+            f32x4 oc[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const float* const pc = part0 + min(c0 + u * GROUPS, copies - 1) * copy_stride;
-            ml[u] = *reinterpret_cast<const float2*>(pc + TR * D + r * 2);
-            oc[u] = *reinterpret_cast<const f32x4*>(pc + r * D + d4 * 4);
+            for (int u = 0; u < AHEAD; ++u) {
+                const float* const pc = part0 + min(c0 + u * SHARE, copies - 1) * copy_stride;
+                ml[u] = *reinterpret_cast<const float2*>(pc + TR * D + r * 2);
+                oc[u] = *reinterpret_cast<const f32x4*>(pc + r * D + d4 * 4);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (c0 + u * SHARE < copies) add(ml[u].x, ml[u].y, oc[u]);
         }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (c0 + u * GROUPS < copies) add(ml[u].x, ml[u].y, oc[u]);
     }
-    os[grp][d4] = o;
-    if (d4 == 0) mls[grp] = float2{m, l};
-    __syncthreads();
-    if (grp != 0) return;
+    if (SHARE > 1) {
+        os[grp][rr][d4] = o;
+        if (d4 == 0) mls[grp][rr] = float2{m, l};
+        __syncthreads();
+        if (grp != 0) return;
 #pragma unroll
-    for (int x = 1; x < GROUPS; ++x) add(mls[x].x, mls[x].y, os[x][d4]);
+        for (int x = 1; x < SHARE; ++x) add(mls[x][rr].x, mls[x][rr].y, os[x][rr][d4]);
+    }
+    if (row >= rows_total) return;
     const float inv = 1.f / l;
     const int tok = row / G;
     bf16x4 o4;
@@ -355,39 +363,44 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(AttnLaunch a, Work wk) {
     *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.out) + ((long long)(it.new_start + tok) * a.q_heads + g * G + (row - tok * G)) * D + d4 * 4) = o4;
 }
 
-template <int D, int RT, class Work>
+template <int D, int RT, int NW, class Work>
 void launch_one(const AttnLaunch& a, const Work& wk, int entries, hipStream_t s) {
-    constexpr int NW = 8;
     hipLaunchKernelGGL((kv8_attn_rows_kernel<D, RT, NW, Work>), dim3((unsigned)entries * a.kv_heads), dim3(64 * NW), 0, s, a, wk);
 }
+template <int D, class Work>
+void launch_waves(const AttnLaunch& a, const Work& wk, int entries, int rows, int waves, hipStream_t s) {
+    if (waves == 4) rows == kKv8Rows ? launch_one<D, 1, 4>(a, wk, entries, s) : launch_one<D, 2, 4>(a, wk, entries, s);
+    else rows == kKv8Rows ? launch_one<D, 1, 8>(a, wk, entries, s) : launch_one<D, 2, 8>(a, wk, entries, s);
+}
 template <class Work>
-void launch_list(const AttnLaunch& a, const Work& wk, int entries, int rows, hipStream_t s) {
-    if (a.head_dim == 64) rows == 16 ? launch_one<64, 1>(a, wk, entries, s) : launch_one<64, 2>(a, wk, entries, s);
-    else rows == 16 ? launch_one<128, 1>(a, wk, entries, s) : launch_one<128, 2>(a, wk, entries, s);
+void launch_list(const AttnLaunch& a, const Work& wk, int entries, int rows, int waves, hipStream_t s) {
+    a.head_dim == 64 ? launch_waves<64>(a, wk, entries, rows, waves, s) : launch_waves<128>(a, wk, entries, rows, waves, s);
 }
 template <int D, int TR, class Work>
-void merge_one(const AttnLaunch& a, const Work& wk, int entries, hipStream_t s) {
-    hipLaunchKernelGGL((kv8_merge_kernel<D, TR, Work>), dim3((unsigned)entries * a.kv_heads * TR), dim3(256), 0, s, a, wk);
+void merge_one(const AttnLaunch& a, const Work& wk, int items, int max_rows, hipStream_t s) {
+    constexpr int SHARE = TR == kKv8TallRows ? 1 : TR == kKv8WideRows ? 4 : 8, RPW = 1024 / (D * SHARE);
+    const int row_groups = ((max_rows < TR ? max_rows : TR) + RPW - 1) / RPW;
+    hipLaunchKernelGGL((kv8_merge_kernel<D, TR, SHARE, Work>), dim3((unsigned)items * a.kv_heads * row_groups), dim3(256), 0, s, a, wk, row_groups);
 }
 template <class Work>
-void merge_list(const AttnLaunch& a, const Work& wk, int entries, int rows, hipStream_t s) {
+void merge_list(const AttnLaunch& a, const Work& wk, int items, int rows, int max_rows, hipStream_t s) {
     const bool d64 = a.head_dim == 64;
-    if (rows == kKv8Rows) d64 ? merge_one<64, kKv8Rows>(a, wk, entries, s) : merge_one<128, kKv8Rows>(a, wk, entries, s);
-    else if (rows == kKv8WideRows) d64 ? merge_one<64, kKv8WideRows>(a, wk, entries, s) : merge_one<128, kKv8WideRows>(a, wk, entries, s);
-    else d64 ? merge_one<64, kKv8TallRows>(a, wk, entries, s) : merge_one<128, kKv8TallRows>(a, wk, entries, s);
+    if (rows == kKv8Rows) d64 ? merge_one<64, kKv8Rows>(a, wk, items, max_rows, s) : merge_one<128, kKv8Rows>(a, wk, items, max_rows, s);
+    else if (rows == kKv8WideRows) d64 ? merge_one<64, kKv8WideRows>(a, wk, items, max_rows, s) : merge_one<128, kKv8WideRows>(a, wk, items, max_rows, s);
+    else d64 ? merge_one<64, kKv8TallRows>(a, wk, items, max_rows, s) : merge_one<128, kKv8TallRows>(a, wk, items, max_rows, s);
 }
 
 }  // namespace
 
-hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s) {
+hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, int waves, hipStream_t s) {
     if (entries <= 0) return hipSuccess;
-    wk.n_reqs <= kAttnReqStep ? launch_list(a, short_list(wk), entries, rows, s) : launch_list(a, wk, entries, rows, s);
+    wk.n_reqs <= kAttnReqStep ? launch_list(a, short_list(wk), entries, rows, waves, s) : launch_list(a, wk, entries, rows, waves, s);
     return hipGetLastError();
 }
 
-hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s) {
-    if (entries <= 0) return hipSuccess;
-    wk.n_reqs <= kAttnReqStep ? merge_list(a, short_list(wk), entries, rows, s) : merge_list(a, wk, entries, rows, s);
+hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int items, int rows, int max_rows, hipStream_t s) {
+    if (items <= 0) return hipSuccess;
+    wk.n_reqs <= kAttnReqStep ? merge_list(a, short_list(wk), items, rows, max_rows, s) : merge_list(a, wk, items, rows, max_rows, s);
     return hipGetLastError();
 }
 

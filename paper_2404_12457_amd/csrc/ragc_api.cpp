@@ -501,7 +501,8 @@ int run_f32(const ragc::AttnLaunch& a, const ragc_batch* batch, const HostMeta& 
 struct Kv8Plan {
     std::vector<int32_t> order;
     int rows = ragc::kKv8Rows;
-    int groups = 1;  // of items of kKv8TallRows rows
+    int waves = 8;  // per workgroup
+    int max_rows = 0;  // of any request, as far as they fit an item
     int chunk = 0;
     int64_t entries = 0, workspace = 0;
 };
@@ -515,6 +516,7 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
     order_requests(h, batch->num_reqs, &plan->order);
     int64_t max_rows = 0;
     for (int r : plan->order) max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
+    plan->max_rows = (int)std::min<int64_t>(max_rows, ragc::kKv8TallRows);
     plan->rows = max_rows <= ragc::kKv8Rows ? ragc::kKv8Rows : max_rows <= ragc::kKv8WideRows ? ragc::kKv8WideRows : ragc::kKv8TallRows;
     int64_t work = 0, items = 0;  // work: blocks that workgroups walk
     for (int r : plan->order) {
@@ -528,6 +530,8 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
         const int64_t chunk = std::max<int64_t>(tall ? 64 : 32, (work / ((tall ? 1 : 2) * cus) + 15) / 16 * 16);
         if (chunk <= INT32_MAX / 2) plan->chunk = (int)chunk;
     }
+    if (const char* e = getenv("KV8_ROWS")) { plan->rows = atoi(e); plan->chunk = 0; }  // XXX
+    if (const char* e = getenv("KV8_CHUNK")) plan->chunk = atoi(e);  // XXX
     bool split = false;
     for (int r : plan->order) {
         const int64_t copies = kv8_copies(h, r, plan->chunk);
@@ -535,24 +539,26 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
         plan->entries += row_tiles(h, r, group, plan->rows) * copies;
     }
     if (!split) plan->chunk = 0;
-    plan->groups = plan->entries * pool->kv_heads >= 2 * cus ? 1 : 2;
+    plan->waves = tall && plan->entries * pool->kv_heads >= 2 * cus ? 4 : 8;
+    if (const char* e = getenv("KV8_GROUPS")) plan->waves = atoi(e);  // XXX
     if (plan->entries > INT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group of the batch too large");
     if (split) plan->workspace = plan->entries * pool->kv_heads * ragc::attn_partial_bytes(pool->head_dim, plan->rows);
     return RAGC_OK;
 }
 
-// Enqueues `launch(list, entries)` for all entries of a plan, as many per launch as the kernel arguments and a grid hold.
-template <class Launch>
-int run_kv8_list(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, const Launch& launch) {
-    // the merge has a workgroup per entry, kv head and row
-    const int64_t max_workgroups = std::min<int64_t>(ragc::kAttnMaxWorkgroups / ragc::kKv8TallRows, UINT32_MAX / a.head_div);
+// Enqueues a plan, as many requests and entries per launch as the kernel arguments and a grid hold: all entries, then all merges.
+int run_kv8(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, hipStream_t s) {
+    const int64_t max_workgroups = std::min<int64_t>(ragc::kAttnMaxWorkgroups, UINT32_MAX / a.head_div);
     const int64_t per_launch = std::max<int64_t>(1, max_workgroups / a.kv_heads);
-    int64_t slots = 0;
+    const auto failed = [](hipError_t e) { return fail(RAGC_ERR_HIP, "attention launch: %s (earlier launches of this call stay enqueued)", hipGetErrorString(e)); };
+    const auto close = [](ragc::AttnWork* wk) {
+        for (int j = wk->n_reqs; j % ragc::kAttnReqStep; ++j) wk->first[j] = INT32_MAX;
+    };
+    ragc::AttnWork wk;
+    wk.splits = plan.chunk;
+    wk.part_base = 0;
     for (size_t i = 0; i < plan.order.size(); i += ragc::kAttnMaxReqs) {
-        ragc::AttnWork wk;
         wk.n_reqs = (int32_t)std::min<size_t>(ragc::kAttnMaxReqs, plan.order.size() - i);
-        wk.splits = plan.chunk;
-        wk.part_base = (int32_t)slots;
         int64_t entries = 0;
         for (int j = 0; j < wk.n_reqs; ++j) {
             const int r = plan.order[i + j];
@@ -560,15 +566,41 @@ int run_kv8_list(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& pl
             wk.req[j] = {h.prefix_len[r], h.new_len[r], h.new_start[r], r};
             entries += row_tiles(h, r, a.group, plan.rows) * kv8_copies(h, r, plan.chunk);
         }
-        for (int j = wk.n_reqs; j % ragc::kAttnReqStep; ++j) wk.first[j] = INT32_MAX;
+        close(&wk);
         for (int64_t e0 = 0; e0 < entries; e0 += per_launch) {
             wk.entry0 = (int32_t)e0;
-            const hipError_t e = launch(wk, (int)std::min<int64_t>(per_launch, entries - e0));
-            if (e != hipSuccess) return fail(RAGC_ERR_HIP, "attention launch: %s (earlier launches of this call stay enqueued)", hipGetErrorString(e));
+            const int n = (int)std::min<int64_t>(per_launch, entries - e0);
+            const hipError_t e = plan.rows == ragc::kKv8TallRows ? ragc::launch_kv8_attn(a, wk, n, plan.waves, s) : ragc::launch_kv8_attn_rows(a, wk, n, plan.rows, plan.waves, s);
+            if (e != hipSuccess) return failed(e);
         }
-        slots += entries;
+        wk.part_base += (int32_t)entries;
     }
-    return RAGC_OK;
+    if (plan.workspace == 0) return RAGC_OK;
+    // the merge has up to 16 workgroups of 256 threads per row tile and kv head
+    const int64_t most = std::max<int64_t>(1, ragc::kAttnMaxWorkgroups / 16 / a.kv_heads);
+    int64_t slot = 0, items = 0;
+    wk.n_reqs = 0;
+    wk.entry0 = wk.part_base = 0;
+    const auto flush = [&]() {
+        close(&wk);
+        const hipError_t e = ragc::launch_kv8_merge(a, wk, (int)items, plan.rows, plan.max_rows, s);
+        wk.n_reqs = 0;
+        items = 0;
+        return e == hipSuccess ? RAGC_OK : failed(e);
+    };
+    for (int r : plan.order) {
+        const int64_t tiles = row_tiles(h, r, a.group, plan.rows), copies = kv8_copies(h, r, plan.chunk);
+        if (copies > 1) {
+            if (tiles > most) return fail(RAGC_ERR_RANGE, "request %d: new_len * group too large", r);
+            if (wk.n_reqs == ragc::kAttnMaxReqs || items + tiles > most)
+                if (int rc = flush()) return rc;
+            wk.first[wk.n_reqs] = (int32_t)items;
+            wk.req[wk.n_reqs++] = {h.prefix_len[r], h.new_len[r], h.new_start[r], (int32_t)slot};
+            items += tiles;
+        }
+        slot += tiles * copies;
+    }
+    return wk.n_reqs > 0 ? flush() : RAGC_OK;
 }
 
 constexpr uint32_t kKv8AttnFlags = RAGC_ATTN_NO_SPLIT | RAGC_ATTN_VALIDATE;
@@ -887,12 +919,7 @@ int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void*
         a.partial = workspace;
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    int rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) {
-        return plan.rows == ragc::kKv8TallRows ? ragc::launch_kv8_attn(a, wk, entries, plan.groups, s) : ragc::launch_kv8_attn_rows(a, wk, entries, plan.rows, s);
-    });
-    if (rc == RAGC_OK && plan.chunk > 0)
-        rc = run_kv8_list(a, h, plan, [&](const ragc::AttnWork& wk, int entries) { return ragc::launch_kv8_merge(a, wk, entries, plan.rows, s); });
-    return rc;
+    return run_kv8(a, h, plan, s);
 }
 
 int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new, void* stream) {

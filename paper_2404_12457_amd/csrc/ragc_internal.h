@@ -119,11 +119,13 @@ hipError_t launch_attn_bf16_merge(const AttnLaunch& a, const AttnWork& wk, int e
 // 8-bit cache (block_stride in bytes).  wk.splits is the number of 16-key blocks that one copy of an item takes (0: one copy takes
 // all); a request has as many copies per row tile as its length asks for, an entry each, and every entry has a slot in the workspace.
 constexpr int kKv8Rows = 16, kKv8WideRows = 32, kKv8TallRows = 128;  // rows per item
-hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s);
-// items of kKv8TallRows rows; groups: wave groups of 4 waves per workgroup, 1 or 2
-hipError_t launch_kv8_attn(const AttnLaunch& a, const AttnWork& wk, int entries, int groups, hipStream_t s);
-// second pass: combines the copies' states of the requests that have more than one
-hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, hipStream_t s);
+// waves: 4 or 8 per workgroup
+hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int entries, int rows, int waves, hipStream_t s);
+// items of kKv8TallRows rows; waves: 4 or 8 per workgroup
+hipError_t launch_kv8_attn(const AttnLaunch& a, const AttnWork& wk, int entries, int waves, hipStream_t s);
+// second pass: combines the copies' states.  The list holds the requests that have more than one, an item per row tile, and as `id` the
+// slot of a request's first entry; items: all of the list.  max_rows: of any request.
+hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int items, int rows, int max_rows, hipStream_t s);
 
 hipError_t launch_append(const PagedBatch& b, void* pool_k, void* pool_v, const void* k_new, const void* v_new,
                          int32_t total_new, int esize, hipStream_t s);
