@@ -325,6 +325,17 @@ int ragc_kv8_append(const ragc_kv_pool* pool, const ragc_batch* batch, const rag
  * Returns a negative ragc_status on error. */
 int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags);
 
+/* Test hook: override how ragc_kv8_attn lays a batch out, process-wide like ragc_debug_set_attn_plan.
+ *   rows   per work item: 0 = library's choice of everything, 16, 32 or 128
+ *   waves  per workgroup: 4 or 8
+ *   chunk  16-key blocks per copy of an item along its keys, a multiple of 16; 0 = items are not split
+ * It changes the workspace size. */
+int ragc_debug_set_kv8_plan(int32_t rows, int32_t waves, int32_t chunk);
+
+/* Test hook: plan[0..2] = rows, waves and chunk that ragc_kv8_attn would choose (all 0 for a batch without new tokens).
+ * Only the host arrays of `batch` are read. */
+int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags, int32_t* plan);
+
 /* Attention of the new tokens of every request over an 8-bit pool, causal, for prompts and for single tokens:
  *     out[t,h,:] = softmax_j( scale * q[t,h,:] . K_j ) V_j ,  j = 0 .. prefix_len+i
  * with every K_j, V_j, those of the new tokens too, from the pool: ragc_kv8_append comes first, on the same stream.

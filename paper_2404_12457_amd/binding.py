@@ -28,6 +28,7 @@ RAGC_SWAP_TO_DEVICE, RAGC_SWAP_TO_HOST = 0, 1
 EXPORTS = ["ragc_version", "ragc_last_error", "ragc_kv_bytes_per_token", "ragc_prefill_attn_workspace",
            "ragc_prefill_attn", "ragc_prefill_attn_static", "ragc_kv_append", "ragc_kv_swap", "ragc_kv_gather",
            "ragc_kv_append_rope", "ragc_kv8_append", "ragc_kv8_attn_workspace", "ragc_kv8_attn",
+           "ragc_debug_set_kv8_plan", "ragc_debug_get_kv8_plan",
            "ragc_batch_validate", "ragc_debug_set_attn_plan", "ragc_debug_get_attn_plan",
            "ragc_debug_set_attn_product", "ragc_debug_get_attn_product"]
 
@@ -94,6 +95,10 @@ def load() -> ctypes.CDLL:
         lib.ragc_kv_append_rope.argtypes = [P, P, P, P, P, P, P, P, I32, P]
         lib.ragc_kv8_append.restype = ctypes.c_int
         lib.ragc_kv8_append.argtypes = [P, P, P, P, P, P, P, I32, P]
+        lib.ragc_debug_set_kv8_plan.restype = ctypes.c_int
+        lib.ragc_debug_set_kv8_plan.argtypes = [I32, I32, I32]
+        lib.ragc_debug_get_kv8_plan.restype = ctypes.c_int
+        lib.ragc_debug_get_kv8_plan.argtypes = [P, P, I32, U32, P]
         lib.ragc_kv8_attn_workspace.restype = I64
         lib.ragc_kv8_attn_workspace.argtypes = [P, P, I32, U32]
         lib.ragc_kv8_attn.restype = ctypes.c_int
@@ -217,6 +222,17 @@ def ragc_kv_append_rope(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_head
 def ragc_kv8_append(pool, batch, rope, q, k_new, v_new, q_out, q_heads: int, stream: int = 0) -> int:
     return _check(load().ragc_kv8_append(_ref(pool), _ref(batch), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
                                          q_heads, stream or None))
+
+
+def ragc_debug_set_kv8_plan(rows: int = 0, waves: int = 8, chunk: int = 0) -> int:
+    return _check(load().ragc_debug_set_kv8_plan(rows, waves, chunk))
+
+
+def ragc_debug_get_kv8_plan(pool, batch, q_heads: int, flags: int = 0) -> Tuple[int, int, int]:
+    """(rows per work item, waves per workgroup, 16-key blocks per copy or 0)"""
+    plan = (ctypes.c_int32 * 3)()
+    _check(load().ragc_debug_get_kv8_plan(_ref(pool), _ref(batch), q_heads, flags, ctypes.addressof(plan)))
+    return tuple(plan)
 
 
 def ragc_kv8_attn_workspace(pool: ragc_kv_pool, batch: ragc_batch, q_heads: int, flags: int = 0) -> int:

@@ -20,6 +20,8 @@ thread_local char g_err[512] = "";
 std::atomic<int> g_force_variant{-1};
 std::atomic<int> g_force_splits{0};
 std::atomic<int> g_force_product{0};
+// that of ragc_debug_set_kv8_plan: chunk << 12 | waves << 8 | rows, 0 = the library decides
+std::atomic<uint32_t> g_force_kv8{0};
 }
 
 namespace ragc {
@@ -512,38 +514,108 @@ inline int64_t kv8_copies(const HostMeta& h, int r, int chunk) {
     return chunk == 0 ? 1 : (blocks + chunk - 1) / chunk;
 }
 
+// The plan is the cheapest of what can run the batch, by a cost model in microseconds with measured constants.  A call takes `start` (launch,
+// prologue, epilogue, and what the first tiles wait for).  A workgroup takes `alone` per 16-key block while it has a CU for itself, `shared`
+// where every CU is busy, and then `each` for its own beginning and end: one that has the CU for itself hides nothing of that.
+// Measured at head_dim 128 (64 in brackets):
+//   16 rows, memory-bound: 64 x (512-2048) keys, 64/8 heads, 8 waves 30.6 us (5.4 TB/s); 128 x (200-1000), 32/8 35 us with 8 waves, 30.4 with
+//     4, of which two workgroups share a CU; one step of 10000 keys, not split, 38.5 with 8, 55 with 4
+//   32 rows: 512 items of 2064 keys 27.3 us with 4 waves, 30.8 with 8; 256 of 4256 keys 31 and 26
+//   128 rows: 256 items of 4224 keys 67 us with 8 waves, 76 with 4 (32 rows: 1024 items, 118); 754 of 400-800 keys 56 and 42
+// Long ranges are also tried in copies of equal length, one per slot, for which a merge has to be paid: a launch and the partial
+// results' way to memory and back (one step of 100003 keys 500 -> 43 us; 4 of 4096, 64/8 heads, 18.6 -> 14).
+struct Kv8Kind {
+    int rows, waves, per_cu;
+    double start, alone, shared, each;
+};
+constexpr Kv8Kind kKv8Kinds[2][6] = {{
+                                         {ragc::kKv8Rows, 8, 1, 8, .055, .19, 1.6},
+                                         {ragc::kKv8Rows, 4, 2, 8, .08, .36, .5},
+                                         {ragc::kKv8WideRows, 8, 1, 8, .07, .08, 4},
+                                         {ragc::kKv8WideRows, 4, 2, 7.5, .11, .157, 2.5},
+                                         {ragc::kKv8TallRows, 8, 1, 10, .227, .227, 4},
+                                         {ragc::kKv8TallRows, 4, 2, 8.5, .3, .45, .5},
+                                     },
+                                     {
+                                         {ragc::kKv8Rows, 8, 1, 8, .05, .1, 1.6},
+                                         {ragc::kKv8Rows, 4, 2, 8, .08, .19, .5},
+                                         {ragc::kKv8WideRows, 8, 1, 8, .06, .06, 4},
+                                         {ragc::kKv8WideRows, 4, 2, 7.5, .075, .09, 2.5},
+                                         {ragc::kKv8TallRows, 8, 1, 9, .133, .133, 4},
+                                         {ragc::kKv8TallRows, 4, 2, 8.5, .17, .28, .5},
+                                     }};
+
+int finish_kv8(const ragc_kv_pool* pool, Kv8Plan* plan) {
+    if (plan->entries > INT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group of the batch too large");
+    if (plan->chunk > 0) plan->workspace = plan->entries * pool->kv_heads * ragc::attn_partial_bytes(pool->head_dim, plan->rows);
+    return RAGC_OK;
+}
+
 int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& h, int group, uint32_t flags, Kv8Plan* plan) {
     order_requests(h, batch->num_reqs, &plan->order);
-    int64_t max_rows = 0;
-    for (int r : plan->order) max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
+    int64_t max_rows = 0, max_blocks = 0;
+    for (int r : plan->order) {
+        max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
+        max_blocks = std::max(max_blocks, kv8_copies(h, r, 1));
+    }
     plan->max_rows = (int)std::min<int64_t>(max_rows, ragc::kKv8TallRows);
-    plan->rows = max_rows <= ragc::kKv8Rows ? ragc::kKv8Rows : max_rows <= ragc::kKv8WideRows ? ragc::kKv8WideRows : ragc::kKv8TallRows;
-    int64_t work = 0, items = 0;  // work: blocks that workgroups walk
-    for (int r : plan->order) {
-        const int64_t tiles = row_tiles(h, r, group, plan->rows) * pool->kv_heads;
-        items += tiles;
-        work += tiles * kv8_copies(h, r, 1);
-    }
     const int64_t cus = cu_count();
-    const bool tall = plan->rows == ragc::kKv8TallRows;
-    if (!(flags & RAGC_ATTN_NO_SPLIT) && (!tall || items < cus)) {
-        const int64_t chunk = std::max<int64_t>(tall ? 64 : 32, (work / ((tall ? 1 : 2) * cus) + 15) / 16 * 16);
-        if (chunk <= INT32_MAX / 2) plan->chunk = (int)chunk;
+    if (const uint32_t forced = g_force_kv8.load(std::memory_order_relaxed)) {  // tests
+        plan->rows = (int)(forced & 0xff);
+        plan->waves = (int)(forced >> 8 & 0xf);
+        plan->chunk = (flags & RAGC_ATTN_NO_SPLIT) || (int64_t)(forced >> 12) >= max_blocks ? 0 : (int)(forced >> 12);
+        for (int r : plan->order) plan->entries += row_tiles(h, r, group, plan->rows) * kv8_copies(h, r, plan->chunk);
+        return finish_kv8(pool, plan);
     }
-    if (const char* e = getenv("KV8_ROWS")) { plan->rows = atoi(e); plan->chunk = 0; }  // XXX
-    if (const char* e = getenv("KV8_CHUNK")) plan->chunk = atoi(e);  // XXX
-    bool split = false;
-    for (int r : plan->order) {
-        const int64_t copies = kv8_copies(h, r, plan->chunk);
-        split |= copies > 1;
-        plan->entries += row_tiles(h, r, group, plan->rows) * copies;
+    double best = -1;
+    int64_t tiles = 0, work = 0;  // items, and blocks that their workgroups walk, of a number of rows
+    int rows = 0;
+    for (const Kv8Kind& k : kKv8Kinds[pool->head_dim == 64]) {
+        if ((k.rows == ragc::kKv8Rows) != (max_rows <= ragc::kKv8Rows)) continue;
+        if (k.rows != rows) {
+            rows = k.rows;
+            tiles = work = 0;
+            for (int r : plan->order) {
+                const int64_t t = row_tiles(h, r, group, rows);
+                tiles += t;
+                work += t * kv8_copies(h, r, 1);
+            }
+        }
+        const int64_t slots = cus * k.per_cu;
+        for (int in_copies = 0; in_copies < 2; ++in_copies) {
+            int64_t chunk = 0, entries = tiles, partials = 0;
+            if (in_copies) {
+                if (flags & RAGC_ATTN_NO_SPLIT) break;
+                chunk = std::max<int64_t>(k.rows == ragc::kKv8TallRows ? 64 : 32, (work * pool->kv_heads / slots + 15) / 16 * 16);
+                if (chunk >= max_blocks) break;
+                entries = 0;
+                for (int r : plan->order) {
+                    const int64_t copies = kv8_copies(h, r, (int)chunk), t = row_tiles(h, r, group, rows);
+                    entries += t * copies;
+                    if (copies > 1) partials += t * copies;
+                }
+            }
+            const int64_t wgs = entries * pool->kv_heads;
+            const double longest = in_copies ? (double)chunk : (double)max_blocks, mean = (double)work / entries;
+            const double filled = (double)wgs / slots;
+            // rounds of one workgroup per CU end together; of two, the later ones run beside what is left of the earlier
+            const double rounds = filled <= 1 ? 1 : k.per_cu > 1 ? filled + .3 / filled : filled <= 4 ? std::ceil(filled) : filled;
+            double cost = k.start + std::max(longest * k.alone, wgs > cus ? rounds * mean * k.shared + (rounds - 1) * k.each
+                                                                          : mean * std::max(k.alone, k.shared * filled));
+            if (in_copies) {
+                const int64_t used = std::min<int64_t>(k.rows, max_rows);
+                cost += 4 + partials * pool->kv_heads * (double)ragc::attn_partial_bytes(pool->head_dim, (int)used) * .7e-6;
+            }
+            if (best < 0 || cost < best) {
+                best = cost;
+                plan->rows = k.rows;
+                plan->waves = k.waves;
+                plan->chunk = (int)chunk;
+                plan->entries = entries;
+            }
+        }
     }
-    if (!split) plan->chunk = 0;
-    plan->waves = tall && plan->entries * pool->kv_heads >= 2 * cus ? 4 : 8;
-    if (const char* e = getenv("KV8_GROUPS")) plan->waves = atoi(e);  // XXX
-    if (plan->entries > INT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group of the batch too large");
-    if (split) plan->workspace = plan->entries * pool->kv_heads * ragc::attn_partial_bytes(pool->head_dim, plan->rows);
-    return RAGC_OK;
+    return finish_kv8(pool, plan);
 }
 
 // Enqueues a plan, as many requests and entries per launch as the kernel arguments and a grid hold: all entries, then all merges.
@@ -889,6 +961,35 @@ int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batc
     Kv8Plan plan;
     if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
     return plan.workspace;
+}
+
+int ragc_debug_set_kv8_plan(int32_t rows, int32_t waves, int32_t chunk) {
+    g_err[0] = 0;
+    if (rows != 0 && rows != ragc::kKv8Rows && rows != ragc::kKv8WideRows && rows != ragc::kKv8TallRows) return fail(RAGC_ERR_SHAPE, "items of %d rows unknown", rows);
+    if (rows != 0 && waves != 4 && waves != 8) return fail(RAGC_ERR_SHAPE, "workgroups of %d waves unknown", waves);
+    if (chunk < 0 || chunk > 0xffff0 || chunk % 16 != 0) return fail(RAGC_ERR_SHAPE, "copies of %d blocks (a multiple of 16 below 2^20)", chunk);
+    g_force_kv8.store(rows == 0 ? 0u : (uint32_t)chunk << 12 | (uint32_t)waves << 8 | (uint32_t)rows, std::memory_order_relaxed);
+    return RAGC_OK;
+}
+
+int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags, int32_t* out) {
+    g_err[0] = 0;
+    if (int rc = check_pool(pool, 1)) return rc;
+    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+    if (!out) return fail(RAGC_ERR_NULL, "plan is NULL");
+    BatchInfo info;
+    HostMeta h;
+    if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
+    out[0] = out[1] = out[2] = 0;
+    if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
+    Kv8Plan plan;
+    if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
+    out[0] = plan.rows;
+    out[1] = plan.waves;
+    out[2] = plan.chunk;
+    return RAGC_OK;
 }
 
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,

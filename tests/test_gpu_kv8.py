@@ -417,3 +417,33 @@ def test_kv8_attention_on_streams_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, _run(c, 0.1))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,waves,chunk", [(r, w, c) for r in (16, 32, 128) for w in (4, 8) for c in (0, 16, 48)])
+def test_kv8_attention_in_every_layout(rows, waves, chunk, d):
+    """Every kernel on lengths that end inside its tiles, split and whole: copies without a key for some rows, and more of them than keys."""
+    c = Case([(700, 37), (15, 1), (0, 130), (1030, 3), (255, 16), (2100, 1)], 8, 2, d, seed=17, pad=1, first_row=1)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        _check(c, d**-0.5)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("rows,waves", [(r, w) for r in (16, 32, 128) for w in (4, 8)])
+def test_kv8_attention_nan_in_every_layout(rows, waves):
+    c = Case([(700, 37), (20, 130)], 8, 2, 128, seed=18)
+    c.fill_prefixes()
+    for at in (3, 20, 36, 37 + 64, 37 + 128):
+        c.v_new[at, 0, 7 * at % 128] = float("nan")
+        c.v_new[at, 1, 127] = float("inf")
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    try:
+        for chunk in (0, 16):
+            B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+            _check(c, 128**-0.5)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)

@@ -211,3 +211,36 @@ def test_kv8_attention_workspace():
     assert _attn_code(pool=p, batch=long) == B.RAGC_ERR_WORKSPACE
     assert _attn_code(pool=p, batch=long, ws=A, n=need - 1) == B.RAGC_ERR_WORKSPACE
     assert _attn_code(pool=p, batch=long, ws=A + 16, n=need) == B.RAGC_ERR_ALIGN
+
+
+def test_kv8_plan_hook():
+    long = _batch(p=(100000,), n=(1,), stride=6251)
+    p = _pool8(num_blocks=7000)
+    try:
+        for bad in ((7, 8, 0), (16, 5, 0), (16, 8, 24), (16, 8, -16), (128, 4, 1 << 20)):
+            assert _code(B.ragc_debug_set_kv8_plan, *bad) == B.RAGC_ERR_SHAPE
+        B.ragc_debug_set_kv8_plan(32, 4, 64)
+        assert B.ragc_debug_get_kv8_plan(p, long, 8) == (32, 4, 64)
+        assert B.ragc_kv8_attn_workspace(p, long, 8) == 98 * 2 * 32 * (128 + 2) * 4  # 6251 blocks in copies of 64, two heads
+        assert B.ragc_debug_get_kv8_plan(p, long, 8, B.RAGC_ATTN_NO_SPLIT) == (32, 4, 0)
+        assert B.ragc_debug_get_kv8_plan(p, _batch(n=(0,)), 8) == (0, 0, 0)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+
+
+def _plan(p, n, hq, hkv, d=128, flags=0):
+    stride = max(-(-(a + b) // 16) for a, b in zip(p, n))
+    return B.ragc_debug_get_kv8_plan(_pool8(num_blocks=1 << 20, kv_heads=hkv, head_dim=d), _batch(p=p, n=n, stride=stride), hq, flags)
+
+
+def test_kv8_plans_of_known_batches():
+    """256 compute units (no GPU here): measured on both sides of the lines."""
+    assert _plan((1000,) * 64, (1,) * 64, 64, 8)[::2] == (16, 0)      # a full batch of decode steps is not split
+    assert _plan((200,) * 64, (1,) * 64, 32, 32) == (16, 4, 0)        # many short workgroups: two per CU
+    rows, _, chunk = _plan((100003,), (1,), 64, 8)                    # one long step is
+    assert rows == 16 and 128 <= chunk <= 512
+    assert _plan((1024,), (100,), 32, 32) [::2] == (32, 0)
+    assert _plan((4096,) * 4, (128,) * 4, 64, 8) == (128, 8, 0)       # an item per CU
+    assert _plan((2000,) * 40, (300,) * 40, 32, 8) == (128, 4, 0)     # many: two workgroups per CU
+    assert _plan((50000,), (64,), 32, 8)[0] == 128 and _plan((50000,), (64,), 32, 8)[2] > 0
+    assert _plan((50000,), (64,), 32, 8, flags=B.RAGC_ATTN_NO_SPLIT)[2] == 0
