@@ -598,10 +598,13 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
             const int64_t wgs = entries * pool->kv_heads;
             const double longest = in_copies ? (double)chunk : (double)max_blocks, mean = (double)work / entries;
             const double filled = (double)wgs / slots;
-            // rounds of one workgroup per CU end together; of two, the later ones run beside what is left of the earlier
-            const double rounds = filled <= 1 ? 1 : k.per_cu > 1 ? filled + .3 / filled : filled <= 4 ? std::ceil(filled) : filled;
-            double cost = k.start + std::max(longest * k.alone, wgs > cus ? rounds * mean * k.shared + (rounds - 1) * k.each
-                                                                          : mean * std::max(k.alone, k.shared * filled));
+            // rounds of one workgroup per CU end together; of two, the later ones run beside what is left of the earlier; memory-bound
+            // ones share one resource whatever the rounds
+            const double rounds = filled <= 1 ? 1 : k.rows == ragc::kKv8Rows ? filled : k.per_cu > 1 ? filled + .3 / filled : filled <= 4 ? std::ceil(filled) : filled;
+            // beyond some thousand blocks each of them is on a page of memory of its own
+            const double alone = k.rows == ragc::kKv8Rows && longest > 1000 ? 1.5 * k.alone : k.alone;
+            double cost = k.start + std::max(longest * alone, wgs > cus ? rounds * mean * k.shared + (rounds - 1) * k.each
+                                                                          : mean * std::max(alone, k.shared * filled));
             if (in_copies) {
                 const int64_t used = std::min<int64_t>(k.rows, max_rows);
                 cost += 4 + partials * pool->kv_heads * (double)ragc::attn_partial_bytes(pool->head_dim, (int)used) * .7e-6;
