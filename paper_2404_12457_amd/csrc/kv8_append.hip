@@ -25,6 +25,7 @@ namespace ragc {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 // |x| of a finite number as a whole number that keeps its order and whether it lies above a border of 20 bits
 __device__ __forceinline__ uint32_t size_key(double x) {
@@ -93,46 +94,76 @@ __device__ __forceinline__ void append_block(const PagedBatch& b, const RopeArgs
     const float* const angles = rope.cos_sin + (long long)(prefix + (int)(row - start)) * rope.rot_dim;
     const int rot = rope.rot_dim, half = rot / 2;  // 0: nothing turns
 
+    // four angles from number i on; rot_dim and the tables make them 16-byte aligned
+    auto four = [&](int i) { return *reinterpret_cast<const f32x4*>(angles + i); };
     double k[NC][16];
     bf16x8 v[NC][2];
     uint32_t key_k = 0, key_v = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int d0 = (cq + 4 * c) * 16 + h * 8;
-            v[c][h] = *reinterpret_cast<const bf16x8*>(src_v + d0);
-            const bf16x8 own = *reinterpret_cast<const bf16x8*>(src_k + d0);
-            double* const out = k[c] + h * 8;
-            if (d0 >= rot) {
+        for (int h = 0; h < 2; ++h) v[c][h] = *reinterpret_cast<const bf16x8*>(src_v + (cq + 4 * c) * 16 + h * 8);
+    if (NC == 2 && rot == D && !rope.interleaved) {
+        // Whole heads by halves, the usual case at head_dim 128: a lane has both ends of its pairs.
 #pragma unroll
-                for (int i = 0; i < 8; ++i) out[i] = (double)(float)own[i];
-            } else if (rope.interleaved) {
+        for (int h = 0; h < 2; ++h) {
+            const int d0 = cq * 16 + h * 8;
+            const bf16x8 lower = *reinterpret_cast<const bf16x8*>(src_k + d0), upper = *reinterpret_cast<const bf16x8*>(src_k + d0 + half);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const f32x4 cs4 = four(d0 + q * 4), sn4 = four(half + d0 + q * 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const double cs = angles[d0 / 2 + i], sn = angles[half + d0 / 2 + i];
-                    const double a = (double)(float)own[2 * i], e = (double)(float)own[2 * i + 1];
-                    out[2 * i] = __builtin_fma(a, cs, -(e * sn));
-                    out[2 * i + 1] = __builtin_fma(a, sn, e * cs);
-                }
-            } else {
-                const bool first = d0 < half;
-                const bf16x8 other = *reinterpret_cast<const bf16x8*>(src_k + (first ? d0 + half : d0 - half));
-                const float* const at = angles + (first ? d0 : d0 - half);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const double cs = at[i], sn = first ? -at[half + i] : at[half + i];
-                    out[i] = __builtin_fma((double)(float)own[i], cs, (double)(float)other[i] * sn);
-                }
-            }
-            if (fresh) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    key_k = max(key_k, size_key(out[i]));
-                    key_v = max(key_v, size_key((double)(float)v[c][h][i]));
+                    const double x = (double)(float)lower[q * 4 + i], y = (double)(float)upper[q * 4 + i], cs = (double)cs4[i], sn = (double)sn4[i];
+                    k[0][h * 8 + q * 4 + i] = __builtin_fma(x, cs, -(y * sn));
+                    k[NC - 1][h * 8 + q * 4 + i] = __builtin_fma(x, sn, y * cs);
                 }
             }
         }
+    } else {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int d0 = (cq + 4 * c) * 16 + h * 8;
+                const bf16x8 own = *reinterpret_cast<const bf16x8*>(src_k + d0);
+                double* const out = k[c] + h * 8;
+                if (d0 >= rot) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[i] = (double)(float)own[i];
+                } else if (rope.interleaved) {
+                    const f32x4 cs = four(d0 / 2), sn = four(half + d0 / 2);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double x = (double)(float)own[2 * i], y = (double)(float)own[2 * i + 1];
+                        out[2 * i] = __builtin_fma(x, (double)cs[i], -(y * (double)sn[i]));
+                        out[2 * i + 1] = __builtin_fma(x, (double)sn[i], y * (double)cs[i]);
+                    }
+                } else {
+                    const bool first = d0 < half;
+                    const bf16x8 other = *reinterpret_cast<const bf16x8*>(src_k + (first ? d0 + half : d0 - half));
+                    const int at = first ? d0 : d0 - half;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const f32x4 cs = four(at + q * 4), sn = four(half + at + q * 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const double turn = (double)(first ? -sn[i] : sn[i]);
+                            out[q * 4 + i] = __builtin_fma((double)(float)own[q * 4 + i], (double)cs[i], (double)(float)other[q * 4 + i] * turn);
+                        }
+                    }
+                }
+            }
+    }
+    if (fresh) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                key_k = max(key_k, size_key(k[c][i]));
+                key_v = max(key_v, size_key((double)(float)v[c][i >> 3][i & 7]));
+            }
+    }
 #pragma unroll
     for (int step = 32; step > 0; step >>= 1) {
         key_k = max(key_k, (uint32_t)__shfl_xor((int)key_k, step, 64));
