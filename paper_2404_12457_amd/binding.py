@@ -58,7 +58,7 @@ class RagcError(RuntimeError):
 
 
 _lib = None
-_calls = None  # C extension: ragc_prefill_attn and ragc_kv_append without ctypes, see the end of this file
+_calls = None  # C extension: the calls of a serving step without ctypes, see the end of this file
 
 
 def load() -> ctypes.CDLL:
@@ -111,7 +111,7 @@ def load() -> ctypes.CDLL:
         if _calls is None:
             _load_calls(warn=True)  # built since this module was imported
         if _calls is not None:
-            _calls.bind(lib, ctypes.cast(lib.ragc_prefill_attn, P).value, ctypes.cast(lib.ragc_kv_append, P).value)
+            _calls.bind(lib, *(ctypes.cast(getattr(lib, f.__name__), P).value for f in _ctypes_calls))
     return _lib
 
 
@@ -259,12 +259,13 @@ def ragc_kv_gather(pool, batch, req: int, length: int, k_out, v_out, stream: int
     return _check(load().ragc_kv_gather(_ref(pool), _ref(batch), req, length, _ptr(k_out), _ptr(v_out), stream or None))
 
 
-_ctypes_calls = ragc_prefill_attn, ragc_kv_append  # what _calls turns to for anything but plain arguments
+# what _calls turns to for anything but plain arguments
+_ctypes_calls = ragc_prefill_attn, ragc_kv_append, ragc_kv_append_rope, ragc_kv8_append, ragc_kv8_attn
 
 
 def _load_calls(warn: bool) -> None:
-    """The two calls through the C extension, if it is there; without it the same functions go through ctypes, 1 us slower."""
-    global _calls, ragc_prefill_attn, ragc_kv_append
+    """Those calls through the C extension, if it is there; without it the same functions go through ctypes, 1 us slower."""
+    global _calls
     importlib.invalidate_caches()  # it may have been built a moment ago
     try:
         calls = importlib.import_module("._calls", __package__)
@@ -272,8 +273,9 @@ def _load_calls(warn: bool) -> None:
         if warn:
             warnings.warn(f"calls go through ctypes: {e}; `python -m paper_2404_12457_amd.build` builds the C extension", RuntimeWarning, 3)
         return
-    calls.setup(globals(), ragc_kv_pool, ragc_batch, _check, *_ctypes_calls)
-    ragc_prefill_attn, ragc_kv_append = calls.ragc_prefill_attn, calls.ragc_kv_append
+    calls.setup(globals(), ragc_kv_pool, ragc_batch, ragc_rope, _check, *_ctypes_calls)
+    for f in _ctypes_calls:
+        globals()[f.__name__] = getattr(calls, f.__name__)
     _calls = calls
 
 

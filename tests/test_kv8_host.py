@@ -244,3 +244,36 @@ def test_kv8_plans_of_known_batches():
     assert _plan((2000,) * 40, (300,) * 40, 32, 8) == (128, 4, 0)     # many: two workgroups per CU
     assert _plan((50000,), (64,), 32, 8)[0] == 128 and _plan((50000,), (64,), 32, 8)[2] > 0
     assert _plan((50000,), (64,), 32, 8, flags=B.RAGC_ATTN_NO_SPLIT)[2] == 0
+
+
+def _outcome(f, *args, **kwargs):
+    try:
+        return f(*args, **kwargs)
+    except B.RagcError as e:
+        return e.code, str(e)
+    except Exception as e:
+        return type(e)
+
+
+_ROWS = [(A,) * 4, (None, A, A, None), (A, None, A, A), (A + 8, A, A, A)]
+
+
+@pytest.mark.parametrize("call", range(2, 5))
+def test_new_calls_marshalled_in_c_behave_as_through_ctypes(call):
+    """Refused or empty calls only: nothing reaches the device."""
+    import inspect
+
+    slow = B._ctypes_calls[call]
+    fast = getattr(B, slow.__name__)
+    assert type(fast).__name__ == "builtin_function_or_method" and inspect.signature(fast).parameters.keys() == inspect.signature(slow).parameters.keys()
+    pool, batch, none = (_pool() if call == 2 else _pool8(k=A + 8)), _batch(p=(60,), n=(10,)), _batch(n=(0,))
+    for b in (batch, none, None, 7):
+        for rope in (_rope(), None, 3):
+            for q, k, v, o in _ROWS:
+                for hq in (8, 7, "8", 2**40):
+                    args = {2: (pool, b, rope, q, k, v, o, None, hq), 3: (pool, b, rope, q, k, v, o, hq), 4: (pool, b, q, o, hq, 0.1)}[call]
+                    for extra in ((), (0,), (None,)) if call != 4 else ((), (0,), (1 << 33,), (0, None, 0, 0)):
+                        assert _outcome(fast, *args, *extra) == _outcome(slow, *args, *extra), (args, extra)
+    assert _outcome(fast) is TypeError and _outcome(fast, *args, nothing=1) is TypeError
+    keys = list(inspect.signature(slow).parameters)
+    assert _outcome(fast, **dict(zip(keys, args))) == _outcome(slow, **dict(zip(keys, args)))
