@@ -18,6 +18,8 @@
 // fourth chunk c from i / 16 on.  V codes turn around in LDS.  Which block: item j of the launch belongs to the largest request
 // r with (new_start[r] - new_start[0] + 30 r) / 16 <= j, which leaves every request room for as many blocks as n tokens can touch
 // from any offset, (n + 30) / 16, so no list has to be made on the host and a captured launch follows the device arrays.
+#include <type_traits>
+
 #include "kv8_codes.h"
 #include "kv_rope.h"
 
@@ -27,17 +29,24 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-// |x| of a finite number as a whole number that keeps its order and whether it lies above a border of 20 bits
+// What is done to K before it is rounded: nothing, every pair of a head of 128 by halves (the usual case: a lane has both ends of
+// its pairs), or any other rotation.  A kernel each: one call's latency is the fetching of its instructions as much as anything.
+enum Turn { kAsItIs, kWholeHalves, kAnyPairs };
+
+// |x| of a finite number as a whole number that keeps its order and whether it lies above a border of 20 bits; 0 for others
 __device__ __forceinline__ uint32_t size_key(double x) {
     const uint64_t b = __double_as_longlong(x);
     const uint32_t hi = (uint32_t)(b >> 32) & 0x7fffffffu;
     return hi >= 0x7ff00000u ? 0u : hi << 1 | ((uint32_t)b != 0);
 }
-// e + 127 for the largest key
+// e + 127 for the largest key: 448 = 1.75 * 2^8
 __device__ __forceinline__ int scale_byte(uint32_t key) {
-    const int e = (int)(key >> 21) - 1023 - 8 + ((key & 0x1fffff) > 0x180000u);  // 448 = 1.75 * 2^8
+    const int e = (int)(key >> 21) - 1023 - 8 + ((key & 0x1fffff) > 0x180000u);
     return key == 0 ? 1 : max(1, min(254, e + 127));
 }
+// the same for the largest |x| in bf16, as its bits
+__device__ __forceinline__ int scale_byte_bf16(uint32_t top) { return max(1, (int)(top >> 7) - 8 + ((top & 0x7f) > 0x60)); }
+
 // fp64 to fp32 towards zero, with the last bit set where something was lost
 __device__ __forceinline__ float round_to_odd(double x) {
     const float f = (float)x;
@@ -53,8 +62,129 @@ __device__ __forceinline__ uint32_t raise4(uint32_t codes, int by) {
     const float x[4] = {__builtin_ldexpf(a[0], by), __builtin_ldexpf(a[1], by), __builtin_ldexpf(b[0], by), __builtin_ldexpf(b[1], by)};
     return encode4(x);
 }
+// the bytes of `held` in N dwords at `at` rounded to a scale 2^-by times theirs; not unrolled: it happens once in a block's life or twice
+__device__ __forceinline__ void raise_held(uint32_t* at, int n, uint32_t held, int by) {
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const uint32_t was = at[i];
+        at[i] = (raise4(was, by) & held) | (was & ~held);
+    }
+}
 
-template <int D>
+// Rows in bf16 that are rounded as they are: a lane's part of a tile, [chunk][half of it].
+template <int NC>
+struct Plain {
+    bf16x8 x[NC][2];
+    __device__ __forceinline__ void load(const __bf16* src, int cq) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[c][h] = *reinterpret_cast<const bf16x8*>(src + (cq + 4 * c) * 16 + h * 8);
+    }
+    // bits of the largest finite |x|, two numbers of 16 bits at a time
+    __device__ __forceinline__ uint32_t top() const {
+        typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
+        u16x8 m = u16x8(0);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u16x8 a = __builtin_bit_cast(u16x8, x[c][h]) & (unsigned short)0x7fff;
+                const u16x8 fine = __builtin_bit_cast(u16x8, a < (unsigned short)0x7f80);  // all bits where it is
+                m = __builtin_elementwise_max(m, a & fine);
+            }
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = max(t, (uint32_t)m[i]);
+        return t;
+    }
+    __device__ __forceinline__ uint32_t codes(int c, int w, int s) const {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf((float)x[c][w >> 1][(w & 1) * 4 + i], 127 - s);
+        return encode4(y);
+    }
+};
+
+// K turned in fp64, which is exact but for the last of 53 bits.
+template <int D, int TURN>
+struct Turned {
+    static constexpr int NC = D / 64;
+    double k[NC][16];
+    __device__ __forceinline__ void load(const __bf16* src, int cq, const float* angles, const RopeArgs& rope) {
+        const int rot = rope.rot_dim, half = rot / 2;
+        // four angles from number i on; rot_dim and the tables make them 16-byte aligned
+        auto four = [&](int i) { return *reinterpret_cast<const f32x4*>(angles + i); };
+        if constexpr (TURN == kWholeHalves) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int d0 = cq * 16 + h * 8;
+                const bf16x8 lower = *reinterpret_cast<const bf16x8*>(src + d0), upper = *reinterpret_cast<const bf16x8*>(src + d0 + D / 2);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const f32x4 cs4 = four(d0 + q * 4), sn4 = four(D / 2 + d0 + q * 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double x = (double)(float)lower[q * 4 + i], y = (double)(float)upper[q * 4 + i], cs = (double)cs4[i], sn = (double)sn4[i];
+                        k[0][h * 8 + q * 4 + i] = __builtin_fma(x, cs, -(y * sn));
+                        k[NC - 1][h * 8 + q * 4 + i] = __builtin_fma(x, sn, y * cs);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int d0 = (cq + 4 * c) * 16 + h * 8;
+                    const bf16x8 own = *reinterpret_cast<const bf16x8*>(src + d0);
+                    double* const out = k[c] + h * 8;
+                    if (d0 >= rot) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) out[i] = (double)(float)own[i];
+                    } else if (rope.interleaved) {
+                        const f32x4 cs = four(d0 / 2), sn = four(half + d0 / 2);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const double x = (double)(float)own[2 * i], y = (double)(float)own[2 * i + 1];
+                            out[2 * i] = __builtin_fma(x, (double)cs[i], -(y * (double)sn[i]));
+                            out[2 * i + 1] = __builtin_fma(x, (double)sn[i], y * (double)cs[i]);
+                        }
+                    } else {
+                        const bool first = d0 < half;
+                        const bf16x8 other = *reinterpret_cast<const bf16x8*>(src + (first ? d0 + half : d0 - half));
+                        const int at = first ? d0 : d0 - half;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const f32x4 cs = four(at + q * 4), sn = four(half + at + q * 4);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const double turn = (double)(first ? -sn[i] : sn[i]);
+                                out[q * 4 + i] = __builtin_fma((double)(float)own[q * 4 + i], (double)cs[i], (double)(float)other[q * 4 + i] * turn);
+                            }
+                        }
+                    }
+                }
+        }
+    }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t = max(t, size_key(k[c][i]));
+        return t;
+    }
+    __device__ __forceinline__ uint32_t codes(int c, int w, int s) const {
+        const double down = __longlong_as_double((long long)(1023 + 127 - s) << 52);
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = round_to_odd(k[c][w * 4 + i] * down);
+        return encode4(y);
+    }
+};
+
+template <int D, int TURN>
 __device__ __forceinline__ void append_block(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, int item, int head, char* lds) {
     constexpr int NC = D / 64;  // 16-element chunks per lane
     const int lane = threadIdx.x & 63, tok = lane & 15, cq = lane >> 4;
@@ -88,125 +218,45 @@ __device__ __forceinline__ void append_block(const PagedBatch& b, const RopeArgs
     const int end = min(kBlock, have + n - i0);
     const bool fresh = tok >= have && tok < end;
     const int blk = b.block_table[(long long)r * b.table_stride + (prefix >> 4) + p];
-    const long long row = start + i0 + max(tok, have) - have < start + n ? start + i0 + max(tok, have) - have : start + n - 1;
+    // lanes without a token of their own take the nearest one's row
+    const int i = i0 + min(max(tok, have), end - 1) - have;
+    const long long row = start + i;
+    Plain<NC> v;
+    v.load(static_cast<const __bf16*>(x.v_new) + (row * b.kv_heads + head) * D, cq);
     const __bf16* const src_k = static_cast<const __bf16*>(x.k_new) + (row * b.kv_heads + head) * D;
-    const __bf16* const src_v = static_cast<const __bf16*>(x.v_new) + (row * b.kv_heads + head) * D;
-    const float* const angles = rope.cos_sin + (long long)(prefix + (int)(row - start)) * rope.rot_dim;
-    const int rot = rope.rot_dim, half = rot / 2;  // 0: nothing turns
-
-    // four angles from number i on; rot_dim and the tables make them 16-byte aligned
-    auto four = [&](int i) { return *reinterpret_cast<const f32x4*>(angles + i); };
-    double k[NC][16];
-    bf16x8 v[NC][2];
-    uint32_t key_k = 0, key_v = 0;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) v[c][h] = *reinterpret_cast<const bf16x8*>(src_v + (cq + 4 * c) * 16 + h * 8);
-    if (NC == 2 && rot == D && !rope.interleaved) {
-        // Whole heads by halves, the usual case at head_dim 128: a lane has both ends of its pairs.
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int d0 = cq * 16 + h * 8;
-            const bf16x8 lower = *reinterpret_cast<const bf16x8*>(src_k + d0), upper = *reinterpret_cast<const bf16x8*>(src_k + d0 + half);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const f32x4 cs4 = four(d0 + q * 4), sn4 = four(half + d0 + q * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const double x = (double)(float)lower[q * 4 + i], y = (double)(float)upper[q * 4 + i], cs = (double)cs4[i], sn = (double)sn4[i];
-                    k[0][h * 8 + q * 4 + i] = __builtin_fma(x, cs, -(y * sn));
-                    k[NC - 1][h * 8 + q * 4 + i] = __builtin_fma(x, sn, y * cs);
-                }
-            }
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int d0 = (cq + 4 * c) * 16 + h * 8;
-                const bf16x8 own = *reinterpret_cast<const bf16x8*>(src_k + d0);
-                double* const out = k[c] + h * 8;
-                if (d0 >= rot) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) out[i] = (double)(float)own[i];
-                } else if (rope.interleaved) {
-                    const f32x4 cs = four(d0 / 2), sn = four(half + d0 / 2);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const double x = (double)(float)own[2 * i], y = (double)(float)own[2 * i + 1];
-                        out[2 * i] = __builtin_fma(x, (double)cs[i], -(y * (double)sn[i]));
-                        out[2 * i + 1] = __builtin_fma(x, (double)sn[i], y * (double)cs[i]);
-                    }
-                } else {
-                    const bool first = d0 < half;
-                    const bf16x8 other = *reinterpret_cast<const bf16x8*>(src_k + (first ? d0 + half : d0 - half));
-                    const int at = first ? d0 : d0 - half;
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const f32x4 cs = four(at + q * 4), sn = four(half + at + q * 4);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const double turn = (double)(first ? -sn[i] : sn[i]);
-                            out[q * 4 + i] = __builtin_fma((double)(float)own[q * 4 + i], (double)cs[i], (double)(float)other[q * 4 + i] * turn);
-                        }
-                    }
-                }
-            }
-    }
-    if (fresh) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                key_k = max(key_k, size_key(k[c][i]));
-                key_v = max(key_v, size_key((double)(float)v[c][i >> 3][i & 7]));
-            }
-    }
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1) {
-        key_k = max(key_k, (uint32_t)__shfl_xor((int)key_k, step, 64));
-        key_v = max(key_v, (uint32_t)__shfl_xor((int)key_v, step, 64));
-    }
+    std::conditional_t<TURN == kAsItIs, Plain<NC>, Turned<D, TURN>> k;
+    if constexpr (TURN == kAsItIs) k.load(src_k, cq);
+    else k.load(src_k, cq, rope.cos_sin + (long long)(prefix + i) * rope.rot_dim, rope);
 
     uint8_t* const base_k = static_cast<uint8_t*>(x.pool_k) + (long long)blk * b.block_stride;
     uint8_t* const base_v = static_cast<uint8_t*>(x.pool_v) + (long long)blk * b.block_stride;
-    uint8_t* const scale_k = base_k + (long long)b.kv_heads * (kBlock * D) + head;
-    uint8_t* const scale_v = base_v + (long long)b.kv_heads * (kBlock * D) + head;
-    uint8_t* const tile_k = base_k + (long long)head * (kBlock * D);
-    uint8_t* const tile_v = base_v + (long long)head * (kBlock * D);
-    int sk = scale_byte(key_k), sv = scale_byte(key_v);
-    int old_k = sk, old_v = sv;
+    const long long scale_at = (long long)b.kv_heads * (kBlock * D) + head, tile_at = (long long)head * (kBlock * D) + lane * 16;
+    int old_k = 0, old_v = 0;
     if (have > 0) {
-        old_k = *scale_k;
-        old_v = *scale_v;
-        sk = max(sk, old_k);
-        sv = max(sv, old_v);
+        old_k = base_k[scale_at];
+        old_v = base_v[scale_at];
     }
+    // the nearest token's row is one of the new ones, so no lane has to be left out
+    uint32_t top_k = k.top(), top_v = v.top();
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) {
+        top_k = max(top_k, (uint32_t)__shfl_xor((int)top_k, step, 64));
+        top_v = max(top_v, (uint32_t)__shfl_xor((int)top_v, step, 64));
+    }
+    const int sk = max(old_k, TURN == kAsItIs ? scale_byte_bf16(top_k) : scale_byte(top_k)), sv = max(old_v, scale_byte_bf16(top_v));
 
     // ---- K: a 16-byte piece per token and chunk
-    const double down_k = __longlong_as_double((long long)(1023 + 127 - sk) << 52);
-    const bool again_k = sk != old_k && tok < have;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        u32x4* const to = reinterpret_cast<u32x4*>(tile_k + c * 1024 + lane * 16);
-        u32x4 codes;
+        u32x4* const to = reinterpret_cast<u32x4*>(base_k + tile_at + c * 1024);
         if (fresh) {
+            u32x4 codes;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = round_to_odd(k[c][w * 4 + i] * down_k);
-                codes[w] = encode4(y);
-            }
+            for (int w = 0; w < 4; ++w) codes[w] = k.codes(c, w, sk);
+            *to = codes;
+        } else if (tok < have && sk != old_k) {
+            raise_held(reinterpret_cast<uint32_t*>(to), 4, ~0u, old_k - sk);
         }
-        if (again_k) {
-            const u32x4 was = *to;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) codes[w] = raise4(was[w], old_k - sk);
-        }
-        if (fresh || again_k) *to = codes;
     }
 
     // ---- V: the codes turn around in LDS, [token][element] with 4 bytes behind each row
@@ -214,61 +264,55 @@ __device__ __forceinline__ void append_block(const PagedBatch& b, const RopeArgs
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            float y[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = __builtin_ldexpf((float)v[c][w >> 1][(w & 1) * 4 + i], 127 - sv);
-            *reinterpret_cast<uint32_t*>(lds + tok * LROW + (cq + 4 * c) * 16 + w * 4) = encode4(y);
-        }
+        for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(lds + tok * LROW + (cq + 4 * c) * 16 + w * 4) = v.codes(c, w, sv);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
     const int t4 = cq * 4;  // this lane's four tokens, element 64 c + 16 w + lane % 16
-    uint32_t mask = 0, held = 0;  // bytes of new tokens, of tokens that are there
+    // bytes of the tokens below `to`
+    auto bytes_to = [&](int to) { return to - t4 >= 4 ? ~0u : to <= t4 ? 0u : (1u << 8 * (to - t4)) - 1; };
+    const uint32_t held = bytes_to(have), mask = bytes_to(end) & ~held;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (t4 + i >= have && t4 + i < end) mask |= 0xffu << 8 * i;
-        if (t4 + i < have) held |= 0xffu << 8 * i;
-    }
-    const bool again_v = sv != old_v && held != 0;
-    if (mask != 0 || again_v) {
+    for (int c = 0; c < NC; ++c) {
+        u32x4* const to = reinterpret_cast<u32x4*>(base_v + tile_at + c * 1024);
+        if (held != 0 && sv != old_v) raise_held(reinterpret_cast<uint32_t*>(to), 4, held, old_v - sv);
+        if (mask == 0) continue;
+        u32x4 codes = u32x4(0);
+        if (mask != ~0u) codes = *to;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            u32x4* const to = reinterpret_cast<u32x4*>(tile_v + c * 1024 + lane * 16);
-            u32x4 codes;
-            if (mask != 0xffffffffu) codes = *to;
+        for (int w = 0; w < 4; ++w) {
+            uint32_t u = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t u = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) u |= (uint32_t)(uint8_t)lds[(t4 + i) * LROW + c * 64 + w * 16 + tok] << 8 * i;
-                if (mask != 0xffffffffu) {
-                    const uint32_t was = again_v ? (raise4(codes[w], old_v - sv) & held) | (codes[w] & ~held) : codes[w];
-                    u = (u & mask) | (was & ~mask);
-                }
-                codes[w] = u;
-            }
-            *to = codes;
+            for (int e = 0; e < 4; ++e) u |= (uint32_t)(uint8_t)lds[(t4 + e) * LROW + c * 64 + w * 16 + tok] << 8 * e;
+            codes[w] = (u & mask) | (codes[w] & ~mask);
         }
+        *to = codes;
     }
     if (lane == 0) {
-        *scale_k = (uint8_t)sk;
-        *scale_v = (uint8_t)sv;
+        base_k[scale_at] = (uint8_t)sk;
+        base_v[scale_at] = (uint8_t)sv;
     }
 }
 
 constexpr int kWaves = 4;
 constexpr int kTurnHeads = 4;
 
-template <int D>
+template <int D, int TURN>
 __global__ __launch_bounds__(64 * kWaves) void kv8_append_kernel(PagedBatch b, RopeArgs rope, RopeRows x, int block_groups, int head_groups, int rows, int q_groups) {
     __shared__ __attribute__((aligned(16))) char lds[kWaves][kBlock * (D + 4)];
     if ((int)blockIdx.x < block_groups) {
         const int w = threadIdx.x >> 6;
         const int head = (int)blockIdx.x % head_groups * kWaves + w;
-        if (head < b.kv_heads) append_block<D>(b, rope, x, __builtin_amdgcn_readfirstlane((int)blockIdx.x / head_groups), __builtin_amdgcn_readfirstlane(head), lds[w]);
+        if (head < b.kv_heads) append_block<D, TURN>(b, rope, x, __builtin_amdgcn_readfirstlane((int)blockIdx.x / head_groups), __builtin_amdgcn_readfirstlane(head), lds[w]);
         return;
     }
-    const int id = (int)blockIdx.x - block_groups;
-    rope_rows<__bf16, kTurnHeads>(b, rope, x, 0, id / q_groups * rows, id % q_groups);
+    if constexpr (TURN != kAsItIs) {
+        const int id = (int)blockIdx.x - block_groups;
+        rope_rows<__bf16, kTurnHeads>(b, rope, x, 0, id / q_groups * rows, id % q_groups);
+    }
+}
+
+template <int D, int TURN>
+void launch_one(const PagedBatch& b, const RopeArgs& rope, const RopeRows& x, int grid, int block_groups, int head_groups, int rows, int q_groups, hipStream_t s) {
+    hipLaunchKernelGGL((kv8_append_kernel<D, TURN>), dim3((unsigned)grid), dim3(64 * kWaves), 0, s, b, rope, x, block_groups, head_groups, rows, q_groups);
 }
 
 }  // namespace
@@ -279,9 +323,10 @@ hipError_t launch_kv8_append(const PagedBatch& b, const RopeArgs& rope, const Ro
     const int rows = 256 / (b.head_dim * 2 / 32), q_groups = (x.q_heads + kTurnHeads - 1) / kTurnHeads;
     const long long blocks = items * head_groups, turns = (long long)((x.total_new + rows - 1) / rows) * q_groups;
     if (blocks + turns > 0xffffff) return hipErrorInvalidValue;  // grid times workgroup size stays below 2^32 threads
-    const dim3 grid((unsigned)(blocks + turns)), block(64 * kWaves);
-    if (b.head_dim == 64) hipLaunchKernelGGL((kv8_append_kernel<64>), grid, block, 0, s, b, rope, x, (int)blocks, head_groups, rows, q_groups);
-    else hipLaunchKernelGGL((kv8_append_kernel<128>), grid, block, 0, s, b, rope, x, (int)blocks, head_groups, rows, q_groups);
+    const int grid = (int)(blocks + turns);
+    const auto launch = [&](auto kernel) { kernel(b, rope, x, grid, (int)blocks, head_groups, rows, q_groups, s); };
+    if (b.head_dim == 64) launch(rope.rot_dim == 0 ? launch_one<64, kAsItIs> : launch_one<64, kAnyPairs>);
+    else launch(rope.rot_dim == 0 ? launch_one<128, kAsItIs> : rope.rot_dim == 128 && !rope.interleaved ? launch_one<128, kWholeHalves> : launch_one<128, kAnyPairs>);
     return hipGetLastError();
 }
 

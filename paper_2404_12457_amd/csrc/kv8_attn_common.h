@@ -8,8 +8,6 @@
 namespace ragc {
 namespace {
 
-constexpr uint32_t kNoNan = 0x7f7f7f7fu;
-
 // Four codes times 2^(s-127), `scale` = that number: exact in bf16 (four bits of mantissa) down to its smallest number, 2^-133.
 __device__ __forceinline__ bf16x4 widen4(uint32_t codes, float scale) {
     const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
@@ -19,8 +17,6 @@ __device__ __forceinline__ bf16x4 widen4(uint32_t codes, float scale) {
 __device__ __forceinline__ bf16x8 join(bf16x4 lo, bf16x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 
-// 0x80 in every byte that is a NaN code
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) { return ((codes & kNoNan) + 0x01010101u) & 0x80808080u; }
 // the codes with NaN made 0, but for the bytes of `except`
 __device__ __forceinline__ uint32_t without_nan(uint32_t codes, uint32_t except = 0) { return codes & (except | ~((nan_bytes(codes) >> 7) * 0xffu)); }
 // 1.0 (0x38) where there is a NaN and 0 elsewhere

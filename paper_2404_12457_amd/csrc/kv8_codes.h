@@ -6,16 +6,16 @@ namespace ragc {
 namespace {
 
 constexpr uint32_t kCodeNan = 0x7f;
+constexpr uint32_t kNoNan = 0x7f7f7f7fu;
 
-// Four numbers to the nearest codes, ties to even; at most 448 in magnitude, or not finite, which gives NaN.
+// 0x80 in every byte that is a NaN code
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) { return ((codes & kNoNan) + 0x01010101u) & 0x80808080u; }
+
+// Four numbers to the nearest codes, ties to even; at most 448 in magnitude, or not finite, which gives NaN (0x7f).
 __device__ __forceinline__ uint32_t encode4(const float* x) {
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
     v = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], v, true);
-    uint32_t u = (uint32_t)v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(__builtin_fabsf(x[i]) <= 448.f)) u = (u & ~(0xffu << 8 * i)) | kCodeNan << 8 * i;
-    return u;
+    return (uint32_t)v & ~nan_bytes((uint32_t)v);
 }
 
 }  // namespace
