@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(AttnLaunch a, Work wk, i
     __shared__ f32x4 os[SHARE][RPW][TPR];
     __shared__ float2 mls[SHARE][RPW];
     const int Hkv = a.kv_heads;
-    const int item = blockIdx.x / (row_groups * Hkv), g = blockIdx.x / row_groups % Hkv;
+    const int item = blockIdx.x / (row_groups * Hkv) + wk.entry0, g = blockIdx.x / row_groups % Hkv;
     const WorkItem it = find_item(wk, item, a.group, TR);
     const int G = a.group, rows_total = it.new_len * G, tiles = (rows_total + TR - 1) / TR;
     const int copies = copies_of(it.prefix + it.new_len, wk.splits);

@@ -558,6 +558,8 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
         max_rows = std::max(max_rows, (int64_t)h.new_len[r] * group);
         max_blocks = std::max(max_blocks, kv8_copies(h, r, 1));
     }
+    // what the kernels' whole numbers and their division by the group hold
+    if (max_rows > 65535LL * ragc::kKv8TallRows || max_rows * group > UINT32_MAX) return fail(RAGC_ERR_RANGE, "new_len * group too large (%lld rows)", (long long)max_rows);
     plan->max_rows = (int)std::min<int64_t>(max_rows, ragc::kKv8TallRows);
     const int64_t cus = cu_count();
     if (const uint32_t forced = g_force_kv8.load(std::memory_order_relaxed)) {  // tests
@@ -655,10 +657,14 @@ int run_kv8(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, h
     const int64_t most = std::max<int64_t>(1, ragc::kAttnMaxWorkgroups / 16 / a.kv_heads);
     int64_t slot = 0, items = 0;
     wk.n_reqs = 0;
-    wk.entry0 = wk.part_base = 0;
+    wk.part_base = 0;
     const auto flush = [&]() {
         close(&wk);
-        const hipError_t e = ragc::launch_kv8_merge(a, wk, (int)items, plan.rows, plan.max_rows, s);
+        hipError_t e = hipSuccess;
+        for (int64_t i0 = 0; i0 < items && e == hipSuccess; i0 += most) {
+            wk.entry0 = (int32_t)i0;
+            e = ragc::launch_kv8_merge(a, wk, (int)std::min(most, items - i0), plan.rows, plan.max_rows, s);
+        }
         wk.n_reqs = 0;
         items = 0;
         return e == hipSuccess ? RAGC_OK : failed(e);
@@ -666,8 +672,7 @@ int run_kv8(const ragc::AttnLaunch& a, const HostMeta& h, const Kv8Plan& plan, h
     for (int r : plan.order) {
         const int64_t tiles = row_tiles(h, r, a.group, plan.rows), copies = kv8_copies(h, r, plan.chunk);
         if (copies > 1) {
-            if (tiles > most) return fail(RAGC_ERR_RANGE, "request %d: new_len * group too large", r);
-            if (wk.n_reqs == ragc::kAttnMaxReqs || items + tiles > most)
+            if (wk.n_reqs == ragc::kAttnMaxReqs)
                 if (int rc = flush()) return rc;
             wk.first[wk.n_reqs] = (int32_t)items;
             wk.req[wk.n_reqs++] = {h.prefix_len[r], h.new_len[r], h.new_start[r], (int32_t)slot};
@@ -788,6 +793,16 @@ int prefill_attn_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const v
     return run_bf16_plan(a, h, plan, s);
 }
 
+// The host side of a call allocates a little; nothing it throws leaves a C entry point.
+template <class F>
+auto guarded(const F& f) noexcept -> decltype(f()) {
+    try {
+        return f();
+    } catch (...) {
+        return fail(RAGC_ERR_HIP, "out of host memory");
+    }
+}
+
 int check_rope(const ragc_rope* rope, const ragc_kv_pool* pool) {
     if (!rope->cos_sin) return fail(RAGC_ERR_NULL, "rope->cos_sin is NULL");
     if (rope->rot_dim < 16 || rope->rot_dim > pool->head_dim || rope->rot_dim % 16 != 0)
@@ -799,7 +814,7 @@ int check_rope(const ragc_rope* rope, const ragc_kv_pool* pool) {
     return RAGC_OK;
 }
 
-// `out` is `in`, or the two do not overlap
+// `out` is `in`, or the rows of the call, `bytes` of them from the same place of either on, do not overlap
 int check_in_place(const void* in, const void* out, int64_t bytes, const char* what) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(out);
     if (a != b && a < b + (uintptr_t)bytes && b < a + (uintptr_t)bytes) return fail(RAGC_ERR_SHAPE, "%s overlaps its input without being it", what);
@@ -828,7 +843,7 @@ int append_rope_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const ra
     if (q_heads > 0 ? !q || !q_out : q || q_out) return fail(RAGC_ERR_NULL, "q and q_out come together, with q_heads above 0, or not at all");
     for (const void* p : {q, k_new, v_new, static_cast<const void*>(q_out), static_cast<const void*>(k_out)})
         if (!aligned16(p)) return fail(RAGC_ERR_ALIGN, "q / k_new / v_new / q_out / k_out must be 16-byte aligned");
-    const int64_t head_bytes = ((int64_t)h.new_start[0] + info.total_new) * pool->head_dim * es;
+    const int64_t head_bytes = info.total_new * pool->head_dim * es;
     if (int rc = check_in_place(q, q_out, q_heads * head_bytes, "q_out")) return rc;
     if (k_out)
         if (int rc = check_in_place(k_new, k_out, pool->kv_heads * head_bytes, "k_out")) return rc;
@@ -915,7 +930,7 @@ int ragc_debug_get_attn_product(const ragc_kv_pool* pool, const ragc_batch* batc
 
 int ragc_batch_validate(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t writes_new_tokens) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool)) return rc;
+    if (int rc = check_pool(pool, -1)) return rc;
     BatchInfo info;
     HostMeta h;
     if (int rc = check_batch(pool, batch, true, true, &h, &info)) return rc;
@@ -953,17 +968,19 @@ int ragc_prefill_attn_static(const ragc_kv_pool* pool, const ragc_batch* batch, 
 
 int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool, 1)) return rc;
-    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
-    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
-        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
-    BatchInfo info;
-    HostMeta h;
-    if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
-    if (batch->num_reqs == 0 || info.total_new == 0) return 0;
-    Kv8Plan plan;
-    if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
-    return plan.workspace;
+    return guarded([&]() -> int64_t {
+        if (int rc = check_pool(pool, 1)) return rc;
+        if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+        if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+            return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+        BatchInfo info;
+        HostMeta h;
+        if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
+        if (batch->num_reqs == 0 || info.total_new == 0) return 0;
+        Kv8Plan plan;
+        if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
+        return plan.workspace;
+    });
 }
 
 int ragc_debug_set_kv8_plan(int32_t rows, int32_t waves, int32_t chunk) {
@@ -977,53 +994,57 @@ int ragc_debug_set_kv8_plan(int32_t rows, int32_t waves, int32_t chunk) {
 
 int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags, int32_t* out) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool, 1)) return rc;
-    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
-    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
-        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
-    if (!out) return fail(RAGC_ERR_NULL, "plan is NULL");
-    BatchInfo info;
-    HostMeta h;
-    if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
-    out[0] = out[1] = out[2] = 0;
-    if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
-    Kv8Plan plan;
-    if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
-    out[0] = plan.rows;
-    out[1] = plan.waves;
-    out[2] = plan.chunk;
-    return RAGC_OK;
+    return guarded([&]() -> int {
+        if (int rc = check_pool(pool, 1)) return rc;
+        if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+        if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+            return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+        if (!out) return fail(RAGC_ERR_NULL, "plan is NULL");
+        BatchInfo info;
+        HostMeta h;
+        if (int rc = check_batch(pool, batch, false, false, &h, &info)) return rc;
+        out[0] = out[1] = out[2] = 0;
+        if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
+        Kv8Plan plan;
+        if (int rc = plan_kv8(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
+        out[0] = plan.rows;
+        out[1] = plan.waves;
+        out[2] = plan.chunk;
+        return RAGC_OK;
+    });
 }
 
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool, 1)) return rc;
-    if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
-    if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
-        return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
-    if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
-        return fail(RAGC_ERR_SHAPE, "softmax_scale must be positive and finite");
-    const bool validate = (flags & RAGC_ATTN_VALIDATE) != 0;
-    BatchInfo info;
-    HostMeta h;
-    if (int rc = check_batch(pool, batch, true, validate, &h, &info)) return rc;
-    if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
-    if (!q || !out) return fail(RAGC_ERR_NULL, "q / out is NULL");
-    if (!aligned16(q) || !aligned16(out)) return fail(RAGC_ERR_ALIGN, "q / out must be 16-byte aligned");
-    if (validate)
-        if (int rc = validate_batch(pool, batch, h, false)) return rc;
-    ragc::AttnLaunch a = make_attn(pool, batch, q, out, q_heads, softmax_scale);
-    Kv8Plan plan;
-    if (int rc = plan_kv8(pool, batch, h, a.group, flags, &plan)) return rc;
-    if (plan.workspace > 0) {
-        if (!workspace || (int64_t)workspace_bytes < plan.workspace)
-            return fail(RAGC_ERR_WORKSPACE, "workspace of %lld bytes needed (ragc_kv8_attn_workspace), %zu given", (long long)plan.workspace, workspace_bytes);
-        if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(RAGC_ERR_ALIGN, "workspace must be 256-byte aligned");
-        a.partial = workspace;
-    }
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    return run_kv8(a, h, plan, s);
+    return guarded([&]() -> int {
+        if (int rc = check_pool(pool, 1)) return rc;
+        if (flags & ~kKv8AttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
+        if (q_heads <= 0 || q_heads % pool->kv_heads != 0)
+            return fail(RAGC_ERR_SHAPE, "q_heads %d not a multiple of kv_heads %d", q_heads, pool->kv_heads);
+        if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+            return fail(RAGC_ERR_SHAPE, "softmax_scale must be positive and finite");
+        const bool validate = (flags & RAGC_ATTN_VALIDATE) != 0;
+        BatchInfo info;
+        HostMeta h;
+        if (int rc = check_batch(pool, batch, true, validate, &h, &info)) return rc;
+        if (batch->num_reqs == 0 || info.total_new == 0) return RAGC_OK;
+        if (!q || !out) return fail(RAGC_ERR_NULL, "q / out is NULL");
+        if (!aligned16(q) || !aligned16(out)) return fail(RAGC_ERR_ALIGN, "q / out must be 16-byte aligned");
+        if (validate)
+            if (int rc = validate_batch(pool, batch, h, false)) return rc;
+        ragc::AttnLaunch a = make_attn(pool, batch, q, out, q_heads, softmax_scale);
+        Kv8Plan plan;
+        if (int rc = plan_kv8(pool, batch, h, a.group, flags, &plan)) return rc;
+        if (plan.workspace > 0) {
+            if (!workspace || (int64_t)workspace_bytes < plan.workspace)
+                return fail(RAGC_ERR_WORKSPACE, "workspace of %lld bytes needed (ragc_kv8_attn_workspace), %zu given", (long long)plan.workspace, workspace_bytes);
+            if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(RAGC_ERR_ALIGN, "workspace must be 256-byte aligned");
+            a.partial = workspace;
+        }
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        return run_kv8(a, h, plan, s);
+    });
 }
 
 int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new, void* stream) {
@@ -1045,17 +1066,21 @@ int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void
 int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
                         const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool)) return rc;
-    if (!rope) return fail(RAGC_ERR_NULL, "rope is NULL (ragc_kv_append stores rows as they are)");
-    return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_heads, stream);
+    return guarded([&]() -> int {
+        if (int rc = check_pool(pool)) return rc;
+        if (!rope) return fail(RAGC_ERR_NULL, "rope is NULL (ragc_kv_append stores rows as they are)");
+        return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, k_out, q_heads, stream);
+    });
 }
 
 int ragc_kv8_append(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
                     const void* v_new, void* q_out, int32_t q_heads, void* stream) {
     g_err[0] = 0;
-    if (int rc = check_pool(pool, 1)) return rc;
-    if (!rope && (q || q_out || q_heads != 0)) return fail(RAGC_ERR_SHAPE, "q without a rope: nothing would be done to it");
-    return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, nullptr, q_heads, stream);
+    return guarded([&]() -> int {
+        if (int rc = check_pool(pool, 1)) return rc;
+        if (!rope && (q || q_out || q_heads != 0)) return fail(RAGC_ERR_SHAPE, "q without a rope: nothing would be done to it");
+        return append_rope_impl(pool, batch, rope, q, k_new, v_new, q_out, nullptr, q_heads, stream);
+    });
 }
 
 int ragc_kv_gather(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t req, int32_t length, void* k_out,

@@ -124,7 +124,7 @@ hipError_t launch_kv8_attn_rows(const AttnLaunch& a, const AttnWork& wk, int ent
 // items of kKv8TallRows rows; waves: 4 or 8 per workgroup
 hipError_t launch_kv8_attn(const AttnLaunch& a, const AttnWork& wk, int entries, int waves, hipStream_t s);
 // second pass: combines the copies' states.  The list holds the requests that have more than one, an item per row tile, and as `id` the
-// slot of a request's first entry; items: all of the list.  max_rows: of any request.
+// slot of a request's first entry; wk.entry0 is the first item of this launch.  max_rows: of any request.
 hipError_t launch_kv8_merge(const AttnLaunch& a, const AttnWork& wk, int items, int rows, int max_rows, hipStream_t s);
 
 hipError_t launch_append(const PagedBatch& b, void* pool_k, void* pool_v, const void* k_new, const void* v_new,

@@ -447,3 +447,84 @@ def test_kv8_attention_nan_in_every_layout(rows, waves):
             _check(c, 128**-0.5)
     finally:
         B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("chunk", [0, 16])
+def test_kv8_attention_of_more_requests_than_an_argument_list_holds(chunk):
+    g = np.random.Generator(np.random.PCG64(19))
+    c = Case([(int(p), int(n)) for p, n in zip(g.integers(0, 700, 200), g.integers(0, 4, 200))], 4, 2, 64, seed=20)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    try:
+        if chunk:
+            B.ragc_debug_set_kv8_plan(16, 8, chunk)
+        _check(c, 0.125)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+
+
+def test_kv8_calls_without_host_arrays_and_with_validation():
+    c = Case([(33, 7), (0, 18)], 8, 2, 128, seed=21)
+    c.fill_prefixes()
+    bare = B.make_batch(2, c.h_table.shape[1], *c.dev, None, None, None, None)  # lengths are read back
+    want = c.appended8(c.host(c.k_new), c.host(c.v_new))
+    B.ragc_kv8_append(c.pool, bare, None, None, c.k_new, c.v_new, None, 0, _stream())
+    for got, w in zip(c.planes, want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    out = torch.empty_like(c.q)
+    B.ragc_kv8_attn(c.pool, bare, c.q, out, 8, 0.1, B.RAGC_ATTN_VALIDATE, None, 0, _stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out, _run(c, 0.1))
+    B.ragc_batch_validate(c.pool, c.batch, True)
+    c.dev[3][1, 0] = c.blocks  # the device's table names a block that does not exist: found before anything is launched
+    with pytest.raises(B.RagcError) as e:
+        B.ragc_kv8_attn(c.pool, c.batch, c.q, out, 8, 0.1, B.RAGC_ATTN_VALIDATE, None, 0, _stream())
+    assert e.value.code == B.RAGC_ERR_RANGE
+    with pytest.raises(B.RagcError):
+        B.ragc_batch_validate(c.pool, c.batch, True)
+
+
+def test_kv8_calls_leave_other_blocks_and_rows_alone():
+    """A batch in the middle of packed arrays and of a pool: nothing outside it changes."""
+    c = Case([(20, 9), (64, 33)], 8, 2, 128, seed=22, pad=2, first_row=4, spare=20)
+    c.fill_prefixes()
+    before = [p.clone() for p in c.planes]
+    cs, keep, rope = _rope(c, 128, False)
+    q = c.q.clone()
+    B.ragc_kv8_append(c.pool, c.batch, rope, c.q, c.k_new, c.v_new, c.q, 8, _stream())  # Q in place
+    out = torch.full((c.rows + 6, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    _run(c, 0.1, out=out)
+    assert torch.all(out[:4] == 7) and torch.all(out[c.rows:] == 7) and torch.equal(c.q[:4], q[:4])
+    used = set()
+    for r, p, n, _ in c.spans():
+        used |= set(c.h_table[r, p // 16:-(-(p + n) // 16)].tolist())
+    others = [b for b in range(c.blocks) if b not in used]
+    for a, b in zip(before, c.planes):
+        assert torch.equal(a[others], b[others]) and torch.equal(a[:, -32:], b[:, -32:])
+
+
+def test_kv8_attention_in_two_graphs_replayed_in_turn():
+    """Two captured calls with workspaces of their own and eager work between their replays."""
+    cases, graphs, outs, spaces = [Case([(2000 + 300 * i, 1), (40, 70)], 8, 2, 128, seed=23 + i) for i in range(2)], [], [], []
+    for c in cases:
+        c.fill_prefixes()
+        B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+        B.ragc_debug_set_kv8_plan(32, 8, 32)
+        need = B.ragc_kv8_attn_workspace(c.pool, c.batch, 8)
+        assert need > 0
+        spaces.append(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        outs.append(torch.empty_like(c.q))
+        torch.cuda.synchronize()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            B.ragc_kv8_attn(c.pool, c.batch, c.q, outs[-1], 8, 0.1, 0, spaces[-1], need, side.cuda_stream)
+        graphs.append(graph)
+    try:
+        for turn in range(3):
+            for c, graph, out in zip(cases, graphs, outs):
+                c.q.normal_()
+                graph.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(out, _run(c, 0.1))
+    finally:
+        B.ragc_debug_set_kv8_plan(0)

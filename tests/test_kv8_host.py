@@ -277,3 +277,19 @@ def test_new_calls_marshalled_in_c_behave_as_through_ctypes(call):
     assert _outcome(fast) is TypeError and _outcome(fast, *args, nothing=1) is TypeError
     keys = list(inspect.signature(slow).parameters)
     assert _outcome(fast, **dict(zip(keys, args))) == _outcome(slow, **dict(zip(keys, args)))
+
+
+def test_rows_that_whole_numbers_do_not_hold_are_refused():
+    big = _batch(p=(0,), n=(1 << 24,), stride=1 << 20)
+    assert _attn_code(pool=_pool8(num_blocks=1 << 21), batch=big, hq=8) == B.RAGC_ERR_RANGE
+    assert _code(B.ragc_kv8_attn_workspace, _pool8(num_blocks=1 << 21), big, 8) == B.RAGC_ERR_RANGE
+    wide = _batch(p=(0,), n=(2000,), stride=200)
+    assert _attn_code(pool=_pool8(kv_heads=1), batch=wide, hq=2048) == B.RAGC_ERR_RANGE
+
+
+def test_an_output_may_stand_right_behind_its_input():
+    """Rows 5.. of a packed array: what lies before them is not the call's.  Refused only for the alignment that comes later."""
+    b = _batch(p=(10,), n=(5,), start=(5, 10))
+    size = 5 * 8 * 128 * 2
+    assert _rope_code(batch=b, qo=A + size - 16) == B.RAGC_ERR_SHAPE
+    assert _rope_code(batch=b, qo=A + size, ko=A + 16) == B.RAGC_ERR_SHAPE and "k_out" in B.ragc_last_error()
