@@ -28,8 +28,10 @@ namespace {
 constexpr int TM = kKv8TallRows;  // rows per work item
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
+// head_dim 64 stays within 128 registers: four waves to a SIMD, for 256 workgroups of eight waves or more 100.8 -> 84 us (32 x (2000+128),
+// 32/8 heads), of four 84.5 -> 81.7.  head_dim 128 holds two.
 template <int D, int NG, class Work>
-__global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(AttnLaunch a, Work wk) {
+__global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_attn_kernel(AttnLaunch a, Work wk) {
     constexpr int TILE = kBlock * D;    // bytes of one head's tile of a block
     constexpr int NC = D / 64;          // pieces of 1 KiB per tile
     constexpr int DB = D / 32;          // 32-column tiles of the output
@@ -282,17 +284,21 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         });
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(0);
-        // V operands two groups ahead, the first ones under the softmax
+        // V operands two groups ahead, the first ones under the softmax; at head_dim 64, where four waves share a SIMD, one ahead and none
+        // in registers over the softmax
         constexpr int VGROUPS = 4 * DB / 2;
-        bf16x8 vbuf[3][2];
+        constexpr int AHEAD = D == 64 ? 1 : 2;
+        bf16x8 vbuf[AHEAD + 1][2];
         auto read_v = [&](auto g_c) {
             constexpr int GI = decltype(g_c)::value;
 #pragma unroll
             for (int x = 0; x < 2; ++x)
-                vbuf[GI % 3][x] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(vst + (2 * GI + x) / DB * (2 * TILE) + (2 * GI + x) % DB * 1024);
+                vbuf[GI % (AHEAD + 1)][x] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>(vst + (2 * GI + x) / DB * (2 * TILE) + (2 * GI + x) % DB * 1024);
         };
-        read_v(std::integral_constant<int, 0>{});
-        read_v(std::integral_constant<int, 1>{});
+        if constexpr (AHEAD > 1) {
+            read_v(std::integral_constant<int, 0>{});
+            read_v(std::integral_constant<int, 1>{});
+        }
         if constexpr (FAST) {
 #pragma unroll
             for (int x = 0; x < NC; ++x) asm volatile("" ::"v"(vreg[x]));  // V has been read: its buffer is free
@@ -344,15 +350,16 @@ __global__ __launch_bounds__(256 * NG, NG == 1 ? 2 : 1) void kv8_attn_kernel(Att
         }
         l_run += psum;
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (AHEAD == 1) read_v(std::integral_constant<int, 0>{});
         __builtin_amdgcn_s_setprio(1);
         static_for<VGROUPS>([&](auto g_c) {
             constexpr int GI = decltype(g_c)::value;
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (GI + 2 < VGROUPS) read_v(std::integral_constant<int, GI + 2>{});
+            if constexpr (GI + AHEAD < VGROUPS) read_v(std::integral_constant<int, GI + AHEAD>{});
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 f32x16& o = oacc[(2 * GI + x) % DB];
-                o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vbuf[GI % 3][x], pb[2 * GI / DB], o, 0, 0, 0);
+                o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vbuf[GI % (AHEAD + 1)][x], pb[2 * GI / DB], o, 0, 0, 0);
             }
         });
         __builtin_amdgcn_sched_barrier(0);

@@ -541,8 +541,8 @@ constexpr Kv8Kind kKv8Kinds[2][6] = {{
                                          {ragc::kKv8Rows, 4, 2, 8, .08, .19, .5},
                                          {ragc::kKv8WideRows, 8, 1, 8, .06, .06, 4},
                                          {ragc::kKv8WideRows, 4, 2, 7.5, .075, .09, 2.5},
-                                         {ragc::kKv8TallRows, 8, 1, 9, .133, .133, 4},
-                                         {ragc::kKv8TallRows, 4, 2, 8.5, .17, .28, .5},
+                                         {ragc::kKv8TallRows, 8, 2, 9, .133, .265, 2.5},
+                                         {ragc::kKv8TallRows, 4, 2, 8.5, .17, .27, .5},
                                      }};
 
 int finish_kv8(const ragc_kv_pool* pool, Kv8Plan* plan) {
@@ -580,7 +580,7 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
             for (int r : plan->order) {
                 const int64_t t = row_tiles(h, r, group, rows);
                 tiles += t;
-                work += t * kv8_copies(h, r, 1);
+                work += t * (h.prefix_len[r] / RAGC_BLOCK_SIZE + 1) + (t + 1) * (h.new_len[r] / RAGC_BLOCK_SIZE) / 2;
             }
         }
         const int64_t slots = cus * k.per_cu;
