@@ -80,7 +80,9 @@
  *   - the fused-append flag is spelled RAGC_ATTN_APPEND_FUSED; RAGC_ATTN_NO_SPLIT is new.
  *   - more exports: ragc_last_error, ragc_kv_bytes_per_token, ragc_prefill_attn_workspace,
  *     ragc_batch_validate, ragc_debug_set_attn_plan, ragc_debug_get_attn_plan,
- *     ragc_prefill_attn_static.
+ *     ragc_prefill_attn_static; for rotated positions and the 8-bit cache ragc_kv_append_rope,
+ *     ragc_kv8_append, ragc_kv8_attn, ragc_kv8_attn_workspace, ragc_debug_set_kv8_plan,
+ *     ragc_debug_get_kv8_plan.
  *   - host copies of the lengths are optional but their absence costs a synchronous
  *     read-back per call (the launch is sized on the host).
  */
