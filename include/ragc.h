@@ -343,9 +343,10 @@ int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, i
  * with every K_j, V_j, those of the new tokens too, from the pool: ragc_kv8_append comes first, on the same stream.
  * Arguments, workspace, lengths under capture and requests without new tokens as for ragc_prefill_attn; q and out are
  * bf16, flags RAGC_ATTN_NO_SPLIT and RAGC_ATTN_VALIDATE.  Softmax and sums are fp32, probabilities are rounded to bf16
- * before the product with V and the output to nearest even; with more than 32 rows (new tokens times q heads per kv
- * head) K is multiplied in 8 bits, which may leave a score off by 2^-12 of scale * sum |q K_j| (8e-6 on unit-variance numbers).  A key or value that a row does not see counts nothing
- * there, whatever its bytes; NaN in one that it sees reaches it. */
+ * before the product with V and the output to nearest even.  Where a request has more than 16 rows (new tokens times q
+ * heads per kv head) the library may multiply K in 8 bits, which leaves a score off by 2^-12 of scale * sum |q K_j| at
+ * most (8e-6 on unit-variance numbers).  A key or value that a row does not see counts nothing there, whatever its
+ * bytes; NaN in one that it sees reaches it. */
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 

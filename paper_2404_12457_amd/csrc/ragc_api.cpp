@@ -517,11 +517,12 @@ inline int64_t kv8_copies(const HostMeta& h, int r, int chunk) {
 // The plan is the cheapest of what can run the batch, by a cost model in microseconds with measured constants.  A call takes `start` (launch,
 // prologue, epilogue, and what the first tiles wait for).  A workgroup takes `alone` per 16-key block while it has a CU for itself, `shared`
 // where every CU is busy, and then `each` for its own beginning and end: one that has the CU for itself hides nothing of that.
-// Measured at head_dim 128 (64 in brackets):
+// Measured, at head_dim 128 where not said otherwise:
 //   16 rows, memory-bound: 64 x (512-2048) keys, 64/8 heads, 8 waves 30.6 us (5.4 TB/s); 128 x (200-1000), 32/8 35 us with 8 waves, 30.4 with
 //     4, of which two workgroups share a CU; one step of 10000 keys, not split, 38.5 with 8, 55 with 4
 //   32 rows: 512 items of 2064 keys 27.3 us with 4 waves, 30.8 with 8; 256 of 4256 keys 31 and 26
 //   128 rows: 256 items of 4224 keys 67 us with 8 waves, 76 with 4 (32 rows: 1024 items, 118); 754 of 400-800 keys 56 and 42
+//   128 rows of 64: 1024 items of 2128 keys 84 us with 8 waves, two workgroups to a CU, 82 with 4; 384 of 2175 40.6 and 44.9
 // Long ranges are also tried in copies of equal length, one per slot, for which a merge has to be paid: a launch and the partial
 // results' way to memory and back (one step of 100003 keys 500 -> 43 us; 4 of 4096, 64/8 heads, 18.6 -> 14).
 struct Kv8Kind {
@@ -570,7 +571,7 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
         return finish_kv8(pool, plan);
     }
     double best = -1;
-    int64_t tiles = 0, work = 0;  // items, and blocks that their workgroups walk, of a number of rows
+    int64_t tiles = 0, work = 0;  // items, and blocks that their workgroups walk (of the new tokens half on average), of a number of rows
     int rows = 0;
     for (const Kv8Kind& k : kKv8Kinds[pool->head_dim == 64]) {
         if ((k.rows == ragc::kKv8Rows) != (max_rows <= ragc::kKv8Rows)) continue;
