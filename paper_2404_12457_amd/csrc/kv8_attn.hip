@@ -150,11 +150,11 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
     lds_char* const v_dst = lds_v + wq * (2 * TILE) + (tg_lane & 1) * 512 + (lane & 15) * 16 + (tg_lane >> 1) * 8;
     const int vis_min = P + div_g(row0) + 1;
     u32x4 vreg[NC];
-    float v_scale;
-    auto read_raw = [&](int step) {
+    uint32_t v_scale;  // and its neighbours
+    auto read_scale = [&](int step) { v_scale = win[256 + window(step) + wq]; };
+    auto read_raw = [&]() {
 #pragma unroll
         for (int x = 0; x < NC; ++x) vreg[x] = *reinterpret_cast<const lds_u32x4*>(v_from + x * 1024);
-        v_scale = scale_of(win[256 + window(step) + wq] >> scale_shift & 255);
     };
     auto check_raw = [&](int step) {
         const int key = (t_lo + step * NG + grp) * 64 + wq * kBlock;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int dt = C * 4 + e;  // elements 16 dt + lane % 16: row (dt / DB) * 16 + lane % 16 of column tile dt % DB
-            *reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(v_dst + tile + (dt % DB) * 1024 + (dt / DB) * 256) = widen4(vreg[C][e], v_scale);
+            *reinterpret_cast<__attribute__((address_space(3))) bf16x4*>(v_dst + tile + (dt % DB) * 1024 + (dt / DB) * 256) = widen4(vreg[C][e], scale_of(v_scale >> scale_shift & 255));
         }
     };
 
@@ -252,7 +252,8 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
             // what the next steps need, before the products: there are one or two such steps in an item
             if (more) {
                 copy_tile(k_src, k_dst + k_next);
-                read_raw(step + 1);
+                read_scale(step + 1);
+                read_raw();
                 check_raw(step + 1);
                 static_for<NC>([&](auto c_c) { store_v(v_next, c_c); });
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read: its buffer is free
@@ -273,11 +274,21 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
                 kbuf[s][sub] = i32x8{(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
             }
         };
+        // the small ones first, so that one trip to LDS brings all that the products and V's conversion start from
+        uint32_t k_raw[2], id_raw = 0;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) k_raw[sub] = win[128 + window(step) + 2 * sub + (l32 >> 4)];
+        if constexpr (FAST) {
+            read_scale(step + 1);
+            id_raw = win[window(step + 2) + wq];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        read_k(0);
+        if constexpr (FAST) read_raw();
+        __builtin_amdgcn_sched_barrier(0);
         int k_scale[2];
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) k_scale[sub] = (int)(win[128 + window(step) + 2 * sub + (l32 >> 4)] >> scale_shift);  // byte 0 counts
-        read_k(0);
-        if constexpr (FAST) read_raw(step + 1);
+        for (int sub = 0; sub < 2; ++sub) k_scale[sub] = (int)(k_raw[sub] >> scale_shift);  // byte 0 counts
         __builtin_amdgcn_s_setprio(1);
         static_for<NC>([&](auto s_c) {
             constexpr int S = decltype(s_c)::value;
@@ -311,7 +322,7 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
         if constexpr (FAST) {
 #pragma unroll
             for (int x = 0; x < NC; ++x) asm volatile("" ::"v"(vreg[x]));  // V has been read: its buffer is free
-            fetch(id_of(step + 2));
+            fetch(__builtin_amdgcn_readfirstlane((int)id_raw));
         }
         if (!FAST && key0 + 64 > wave_vis_min) {
 #pragma unroll
@@ -377,7 +388,8 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
 
     if (nsteps > 0) {
         wait_vmcnt<0>();
-        read_raw(0);
+        read_scale(0);
+        read_raw();
         block_barrier();  // nan_seen is 0
         check_raw(0);
         static_for<NC>([&](auto c_c) { store_v(0, c_c); });
