@@ -22,13 +22,14 @@
 // row's reference exponent is raised only when a tile's probabilities against it sum to more than 2^8.
 //
 // What bounds it: matrix and vector units, of which the waves of a SIMD use one after the other more than side by side: of a CU's busy time
-// the products take 0.51, vector instructions 0.47 (16 ragged requests, 32/8 heads of 128: 238 us, 1020 TFLOP/s of the 1236 that a large bf16
+// the products take 0.52, vector instructions 0.47 (16 ragged requests, 32/8 heads of 128: 233 us, 1036 TFLOP/s of the 1236 that a large bf16
 // product reaches; the bf16 cache's kernel takes 289 for such a batch).  4 x (4096+128), 64/8 heads: 67 us, 1030 TFLOP/s.  A step of
 // eight waves takes 4215 cycles at head_dim 128: 1090 for the scores, 1300 for softmax and V's conversion, 550 for P V as a wave sees them, and 1160 until its
 // sister on the SIMD is done; the products of both need 2048.  At head_dim 64 the vector part is twice the products.
 // What is brought for later steps is issued under the products: without a branch 71 instead of 77 us (4 x (4096+128)), and
 // a wave in its products goes before one in its softmax (s_setprio): 69.  Measured within 2 % or slower: the scores of the next step
-// among the softmax of this one, wave groups half a step apart, copies two steps ahead, K or V operands further ahead.
+// among the softmax of this one, wave groups half a step apart, copies two steps ahead, K or V operands further ahead, row sums by
+// fp32 adds or by products with ones.
 #include "kv8_attn_common.h"
 
 namespace ragc {
@@ -271,6 +272,7 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
             for (int sub = 0; sub < 2; ++sub) {
                 const u32x4 k0 = *reinterpret_cast<const lds_u32x4*>(kst + sub * 2 * TILE + s * 1024);
                 const u32x4 k1 = *reinterpret_cast<const lds_u32x4*>(kst + sub * 2 * TILE + s * 1024 + 256);
+                if (s == 0) __builtin_amdgcn_sched_barrier(0);  // the first product's operands arrive first
                 kbuf[s][sub] = i32x8{(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
             }
         };
@@ -351,7 +353,7 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
             weigh(m_run);
             raise_any = __builtin_amdgcn_ballot_w64(!(psum <= kRaiseSum)) != 0;
         }
-        if (raise_any) {
+        if (__builtin_expect(raise_any, false)) {
             float mx = sacc[0][0];
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub)
