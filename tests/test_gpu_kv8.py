@@ -528,3 +528,60 @@ def test_kv8_attention_in_two_graphs_replayed_in_turn():
                 assert torch.equal(out, _run(c, 0.1))
     finally:
         B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("dtype", ["e4m3", "bf16"])
+def test_blocks_behind_the_first_four_gib_of_a_plane(dtype):
+    """The same blocks 128 MiB apart: offsets that 32 bits do not hold, in every call and kernel."""
+    c = Case([(200, 17), (300, 1), (61, 40)], 8, 2, 128, dtype, seed=29)
+    if dtype == "e4m3":
+        c.fill_prefixes()
+    size, stride = c.planes[0].element_size(), (1 << 27) // c.planes[0].element_size()
+    assert int(c.h_table.max()) * (1 << 27) > 1 << 32
+    far = [torch.empty(c.blocks * stride, dtype=p.dtype, device="cuda").view(c.blocks, stride) for p in c.planes]
+    for f, p in zip(far, c.planes):
+        f[:, :c.stride] = p
+    pool = B.make_pool(*far, c.blocks, 2, 128, c.pool.dtype, stride)
+    cs, keep, rope = _rope(c, 128, False)
+    q_out = [torch.empty_like(c.q) for _ in range(2)]
+    for p, q in zip((c.pool, pool), q_out):
+        if dtype == "e4m3":
+            B.ragc_kv8_append(p, c.batch, rope, c.q, c.k_new, c.v_new, q, 8, _stream())
+        else:
+            B.ragc_kv_append_rope(p, c.batch, rope, c.q, c.k_new, c.v_new, q, None, 8, _stream())
+    torch.cuda.synchronize()
+    bits = torch.uint8 if size == 1 else torch.int16
+    assert torch.equal(q_out[0].view(torch.int16), q_out[1].view(torch.int16))
+    for f, p in zip(far, c.planes):
+        assert torch.equal(f[:, :c.stride].contiguous().view(bits), p.contiguous().view(bits))
+    if dtype == "bf16":
+        return
+    try:
+        for plan in [(16, 8, 0), (16, 4, 16), (32, 4, 0), (128, 4, 0), (128, 8, 16)]:
+            B.ragc_debug_set_kv8_plan(*plan)
+            need = B.ragc_kv8_attn_workspace(c.pool, c.batch, 8)
+            ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+            outs = [torch.empty_like(c.q) for _ in range(2)]
+            for p, o in zip((c.pool, pool), outs):
+                B.ragc_kv8_attn(p, c.batch, q_out[0], o, 8, 0.1, 0, ws, need, _stream())
+            torch.cuda.synchronize()
+            assert not torch.isnan(outs[0]).any() and torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("rows,waves,chunk", [(16, 4, 0), (16, 8, 16), (32, 4, 16), (128, 4, 0), (128, 8, 0), (128, 8, 16)])
+@pytest.mark.filterwarnings("ignore:invalid value")
+def test_kv8_attention_rows_of_q_that_are_not_finite_stay_alone(rows, waves, chunk):
+    c = Case([(300, 40), (17, 1), (0, 3)], 8, 2, 64, seed=31)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    c.q[3, 1, 5] = float("nan")
+    c.q[20, 7, 60] = float("inf")
+    c.q[40, 0, 0] = -float("inf")
+    c.q[42, 2, :] = 0.0
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        _check(c, 0.125)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
