@@ -524,7 +524,8 @@ inline int64_t kv8_copies(const HostMeta& h, int r, int chunk) {
 //   128 rows: 256 items of 4224 keys 67 us with 8 waves, 76 with 4 (32 rows: 1024 items, 118); 754 of 400-800 keys 56 and 42
 //   128 rows of 64: 1024 items of 2128 keys 84 us with 8 waves, two workgroups to a CU, 82 with 4; 384 of 2175 40.6 and 44.9
 // Long ranges are also tried in copies of equal length, one per slot, for which a merge has to be paid: a launch and the partial
-// results' way to memory and back (one step of 100003 keys 500 -> 43 us; 4 of 4096, 64/8 heads, 18.6 -> 14).
+// results' way to memory and back (one step of 100003 keys 500 -> 43 us; 4 of 4096, 64/8 heads, 18.6 -> 14; a prompt of 8000+300, 32/8 heads,
+// in items of 128 rows 112 -> 56, of 64 numbers a head 76 -> 40).
 struct Kv8Kind {
     int rows, waves, per_cu;
     double start, alone, shared, each;
@@ -542,8 +543,8 @@ constexpr Kv8Kind kKv8Kinds[2][6] = {{
                                          {ragc::kKv8Rows, 4, 2, 8, .08, .19, .5},
                                          {ragc::kKv8WideRows, 8, 1, 8, .06, .06, 4},
                                          {ragc::kKv8WideRows, 4, 2, 7.5, .075, .09, 2.5},
-                                         {ragc::kKv8TallRows, 8, 2, 9, .133, .265, 2.5},
-                                         {ragc::kKv8TallRows, 4, 2, 8.5, .17, .27, .5},
+                                         {ragc::kKv8TallRows, 8, 2, 9, .133, .265, 1.5},
+                                         {ragc::kKv8TallRows, 4, 2, 8.5, .17, .28, .5},
                                      }};
 
 int finish_kv8(const ragc_kv_pool* pool, Kv8Plan* plan) {
@@ -585,32 +586,58 @@ int plan_kv8(const ragc_kv_pool* pool, const ragc_batch* batch, const HostMeta& 
             }
         }
         const int64_t slots = cus * k.per_cu;
-        for (int in_copies = 0; in_copies < 2; ++in_copies) {
-            int64_t chunk = 0, entries = tiles, partials = 0;
-            if (in_copies) {
-                if (flags & RAGC_ATTN_NO_SPLIT) break;
-                chunk = std::max<int64_t>(k.rows == ragc::kKv8TallRows ? 64 : 32, (work * pool->kv_heads / slots + 15) / 16 * 16);
-                if (chunk >= max_blocks) break;
+        // lengths of a copy to look at: none, one copy per slot; of 128 rows also one per CU or two, and each with the longest request in
+        // one copy less
+        const bool tall = k.rows == ragc::kKv8TallRows;
+        int64_t chunks[5] = {0}, lengths = 1;
+        const auto ceil16 = [](int64_t x) { return (x + 15) / 16 * 16; };
+        if (flags & RAGC_ATTN_NO_SPLIT) {
+        } else if (!tall) {
+            chunks[lengths++] = std::max<int64_t>(32, ceil16(work * pool->kv_heads / slots));
+        } else if (tiles * pool->kv_heads < slots) {
+            for (const int64_t wanted : {slots, k.per_cu > 1 ? cus : 2 * slots}) {
+                const int64_t copies = (max_blocks - 1) / std::max<int64_t>(64, work * pool->kv_heads / wanted) + 1;
+                for (int64_t n = copies; n > 1 && n >= copies - 1; --n) chunks[lengths++] = std::max<int64_t>(64, ceil16((max_blocks - 1) / n + 1));
+            }
+        }
+        for (int c = 0; c < lengths; ++c) {
+            const int64_t chunk = chunks[c];
+            int64_t entries = tiles, partials = 0, last = 0;  // last: blocks of any row tile's last copy
+            if (chunk > 0) {
+                if (chunk >= max_blocks) continue;
                 entries = 0;
                 for (int r : plan->order) {
                     const int64_t copies = kv8_copies(h, r, (int)chunk), t = row_tiles(h, r, group, rows);
                     entries += t * copies;
                     if (copies > 1) partials += t * copies;
+                    last = std::max(last, kv8_copies(h, r, 1) % chunk + h.new_len[r] / RAGC_BLOCK_SIZE);
                 }
             }
             const int64_t wgs = entries * pool->kv_heads;
-            const double longest = in_copies ? (double)chunk : (double)max_blocks, mean = (double)work / entries;
             const double filled = (double)wgs / slots;
-            // rounds of one workgroup per CU end together; of two, the later ones run beside what is left of the earlier; memory-bound
-            // ones share one resource whatever the rounds
-            const double rounds = filled <= 1 ? 1 : k.rows == ragc::kKv8Rows ? filled : k.per_cu > 1 ? filled + .3 / filled : filled <= 4 ? std::ceil(filled) : filled;
-            // beyond some thousand blocks each of them is on a page of memory of its own
-            const double alone = k.rows == ragc::kKv8Rows && longest > 1000 ? 1.5 * k.alone : k.alone;
-            double cost = k.start + std::max(longest * alone, wgs > cus ? rounds * mean * k.shared + (rounds - 1) * k.each
-                                                                          : mean * std::max(alone, k.shared * filled));
-            if (in_copies) {
+            double cost;
+            if (tall && chunk > 0) {
+                // Copies are equal, but for the last of each row tile.  Whole rounds of them, as much as the work makes; the last round has CUs
+                // with one workgroup or two, where last copies count unless they are short; those that no round has room for come behind it.
+                const double full = (double)work * pool->kv_heads / chunk / slots, whole = std::floor(full);
+                const double rest = (2 * last > chunk ? std::max(full, std::min(filled, std::ceil(full))) : full) - whole;
+                cost = k.start + whole * (chunk * k.shared + k.each);
+                if (rest > 0) cost += k.each + chunk * (k.per_cu > 1 && rest > .5 ? k.shared : k.alone);
+                if (std::ceil(filled) > std::ceil(full)) cost += std::min(chunk, last) * k.alone;
+            } else {
+                const double longest = chunk > 0 ? (double)chunk : (double)max_blocks, mean = (double)work / entries;
+                // rounds of one workgroup per CU end together; of two, the later ones run beside what is left of the earlier; memory-bound
+                // ones share one resource whatever the rounds
+                const double rounds = filled <= 1 ? 1 : k.rows == ragc::kKv8Rows ? filled : k.per_cu > 1 ? filled + .3 / filled : filled <= 4 ? std::ceil(filled) : filled;
+                // beyond some thousand blocks each of them is on a page of memory of its own
+                const double alone = k.rows == ragc::kKv8Rows && longest > 1000 ? 1.5 * k.alone : k.alone;
+                cost = k.start + std::max(longest * alone, wgs > cus ? rounds * mean * k.shared + (rounds - 1) * k.each
+                                                                     : mean * std::max(alone, k.shared * filled));
+            }
+            if (chunk > 0) {
+                // few rows: what the partial results cost on both sides; 128: the merge alone, the rest is in the figures above
                 const int64_t used = std::min<int64_t>(k.rows, max_rows);
-                cost += 4 + partials * pool->kv_heads * (double)ragc::attn_partial_bytes(pool->head_dim, (int)used) * .7e-6;
+                cost += 4 + partials * pool->kv_heads * (double)ragc::attn_partial_bytes(pool->head_dim, (int)used) * (tall ? .15e-6 : .7e-6);
             }
             if (best < 0 || cost < best) {
                 best = cost;

@@ -246,6 +246,15 @@ def test_kv8_plans_of_known_batches():
     assert _plan((50000,), (64,), 32, 8, flags=B.RAGC_ATTN_NO_SPLIT)[2] == 0
 
 
+def test_kv8_plans_of_few_long_prompts():
+    """Copies of equal length that the compute units hold at once: one more of them per row tile would be a second round."""
+    rows, waves, chunk = _plan((8000,), (300,), 32, 8)
+    copies = -(-(8300 // 16 + 1) // chunk)
+    assert (rows, waves) == (128, 8) and 10 * 8 * copies <= 256 < 10 * 8 * (copies + 1)
+    assert _plan((8000, 8000), (200, 200), 32, 8)[2] > 0 and _plan((16000,), (100,), 64, 8)[2] > 0
+    assert _plan((8000,) * 40, (200,) * 40, 32, 8)[2] == 0  # a full batch is whole
+
+
 def _outcome(f, *args, **kwargs):
     try:
         return f(*args, **kwargs)
