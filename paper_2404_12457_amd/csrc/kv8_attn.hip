@@ -135,8 +135,10 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
         copy_tile(uniform_u64(pool_v + at), lds_addr(raw_v));
     };
     auto id_of = [&](int step) { return __builtin_amdgcn_readfirstlane((int)win[window(step) + wq]); };
-    // the next window: ids early in this one, scales when those are there
+    // the next window, where there is a step for it: ids early in this one, scales when those are there.  More steps of this window
+    // follow either copy, the first of which waits for it.
     auto next_window = [&](int step) {
+        if ((step | 15) + 1 >= nsteps) return;
         const int to = ((step >> 4 & 1) ^ 1) * 64;
         if ((step & 15) == 2) dma_4B_per_lane(table + block_of((step | 15) + 1), lds_addr(win + to));
         if ((step & 15) == 6) {
@@ -405,10 +407,12 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
         for (; step < nsteps; ++step) do_step(step, std::false_type{});
     }
 
-    // ---- merge the wave groups through LDS (nothing is under way to it any more)
+    // ---- merge the wave groups through LDS.  The copies' areas are reused: none is under way, as each was asked for by a step before
+    // the last; the wait is there for those who change that, and costs nothing.
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
     lds_char* const lds = (lds_char*)smem;
     auto piece = [&](int t, int q) { return f32x4{oacc[t][q * 4], oacc[t][q * 4 + 1], oacc[t][q * 4 + 2], oacc[t][q * 4 + 3]}; };
+    wait_vmcnt<0>();
     block_barrier();  // every wave is done with the tiles: their memory is reused below
     if (nan_seen) {
         // The keys of the frontier once more: a row that sees a NaN has it in the output.

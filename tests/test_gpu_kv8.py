@@ -585,3 +585,22 @@ def test_kv8_attention_rows_of_q_that_are_not_finite_stay_alone(rows, waves, chu
         _check(c, 0.125)
     finally:
         B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("steps", [3, 7, 16, 17, 19, 23])
+def test_kv8_attention_key_loops_that_end_anywhere_in_a_window(steps, split, d):
+    """128 rows, two wave groups, a tile of 64 keys each per step: loops that end where block ids or scales of steps 16 on would be
+    asked for (3, 7, 19, 23) and around the change of windows, with and without a last tile for the second group; whole and as the last copy."""
+    chunk = 16 * -(-steps // 2) if split else 0  # blocks: at least as many steps as the last copy has
+    keys = [16 * chunk + 128 * steps, 16 * chunk + 128 * steps - 64 - 9]
+    c = Case([(k - n, n) for k, n in zip(keys, (40, 33))], 8, 2, d, seed=steps)
+    c.fill_prefixes()
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    try:
+        B.ragc_debug_set_kv8_plan(128, 8, chunk)
+        assert B.ragc_debug_get_kv8_plan(c.pool, c.batch, 8) == (128, 8, chunk)
+        _check(c, d**-0.5)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
