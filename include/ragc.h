@@ -346,7 +346,9 @@ int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, i
  * before the product with V and the output to nearest even.  Where a request has more than 16 rows (new tokens times q
  * heads per kv head) the library may multiply K in 8 bits, which leaves a score off by 2^-12 of scale * sum |q K_j| at
  * most (8e-6 on unit-variance numbers).  A key or value that a row does not see counts nothing there, whatever its
- * bytes; NaN in one that it sees reaches it. */
+ * bytes; NaN in one that it sees reaches it.  A value of 2^128 or more, which ragc_kv8_append makes of bf16 numbers from 1.9375 * 2^127 on, is
+ * an infinity, and the column of a row that sees it an infinity or NaN; weights of up to 2^8 come before the division, so sums may overflow
+ * from 2^120 / keys on. */
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 

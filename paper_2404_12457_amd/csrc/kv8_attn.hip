@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
     constexpr int WSTRIDE = (DB * 4 + 1) * 64 * 16;  // bytes per wave in the merge area: [DB*4 + 1][64 lanes] of 16
     static_assert(NG == 1 ? 4 * 32 * OROWB <= GROUPB : 4 * WSTRIDE <= NG * GROUPB && 32 * OROWB <= WSTRIDE, "merge area and output patches");
     __shared__ __attribute__((aligned(1024))) char smem[NG * GROUPB];
-    __shared__ int nan_seen;  // a NaN has been taken out of a V that not every row of the item sees
+    __shared__ int nan_seen;  // a number that is not finite has been taken out of a V that not every row of the item sees
 
     touch_args(a, wk);
     const int Hkv = a.kv_heads;
@@ -162,17 +162,17 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
     auto check_raw = [&](int step) {
         const int key = (t_lo + step * NG + grp) * 64 + wq * kBlock;
         if (key + kBlock > vis_min) {
-            // The frontier: slots behind the last visible key may hold anything and become 0.  NaN in a key that some rows see and
-            // others do not would reach all through probabilities of 0: it becomes 0, and is given to its rows at the end.
-            const uint32_t keep = below(key + tg_lane * 4, kv_limit);
+            // The frontier: slots behind the last visible key may hold anything and become 0.  What bf16 does not hold, in a key that some
+            // rows see and others do not, would reach all through probabilities of 0: it becomes 0, and NaN is given to its rows at the end.
+            const uint32_t keep = below(key + tg_lane * 4, kv_limit), to_top = not_finite_from(v_scale >> scale_shift & 255);
             uint32_t nan = 0;
 #pragma unroll
             for (int x = 0; x < NC; ++x)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     vreg[x][e] &= keep;
-                    nan |= nan_bytes(vreg[x][e]);
-                    vreg[x][e] = without_nan(vreg[x][e], below(key + tg_lane * 4, vis_min));
+                    nan |= nan_bytes(vreg[x][e], to_top);
+                    vreg[x][e] = without_nan(vreg[x][e], to_top, below(key + tg_lane * 4, vis_min));
                 }
             if (nan != 0) nan_seen = 1;
         }
@@ -415,15 +415,17 @@ __global__ __launch_bounds__(256 * NG, D == 64 ? 4 : NG == 1 ? 2 : 1) void kv8_a
     wait_vmcnt<0>();
     block_barrier();  // every wave is done with the tiles: their memory is reused below
     if (nan_seen) {
-        // The keys of the frontier once more: a row that sees a NaN has it in the output.
+        // The keys of the frontier once more: a row that sees what was taken out has NaN in the output.
         for (int key = vis_min; key < my_vis; ++key) {
-            const uint8_t* const tile = pool_v + (long long)table[key >> 4] * a.block_stride + (long long)g * TILE;
+            const uint8_t* const block = pool_v + (long long)table[key >> 4] * a.block_stride;
+            const uint8_t* const tile = block + (long long)g * TILE;
+            const uint32_t to_top = not_finite_from(block[(long long)Hkv * TILE + g]);
 #pragma unroll
             for (int t = 0; t < DB; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int m = (i >> 2) * 8 + kg * 4 + (i & 3), d = (D / 2) * (m >> 4) + 16 * t + (m & 15);
-                    if ((tile[(((d >> 6) * 4 + ((key & 15) >> 2)) * 16 + (d & 15)) * 16 + ((d & 63) >> 4) * 4 + (key & 3)] & kCodeNan) == kCodeNan) oacc[t][i] = __builtin_nanf("");
+                    if (nan_bytes(tile[(((d >> 6) * 4 + ((key & 15) >> 2)) * 16 + (d & 15)) * 16 + ((d & 63) >> 4) * 4 + (key & 3)], to_top & 0xff) & 0x80) oacc[t][i] = __builtin_nanf("");
                 }
         }
     }

@@ -17,10 +17,15 @@ __device__ __forceinline__ bf16x4 widen4(uint32_t codes, float scale) {
 __device__ __forceinline__ bf16x8 join(bf16x4 lo, bf16x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 
-// the codes with NaN made 0, but for the bytes of `except`
-__device__ __forceinline__ uint32_t without_nan(uint32_t codes, uint32_t except = 0) { return codes & (except | ~((nan_bytes(codes) >> 7) * 0xffu)); }
-// 1.0 (0x38) where there is a NaN and 0 elsewhere
-__device__ __forceinline__ uint32_t where_nan(uint32_t codes) { return (nan_bytes(codes) >> 7) * 0x38u; }
+// What bf16 does not hold of a block with scale byte s, as `to_top` of nan_bytes: NaN, and numbers of 2^128 or more, which are the codes
+// from exponent 262 - s on (there are none up to s = 246).
+__device__ __forceinline__ uint32_t not_finite_from(int s) { return (uint32_t)(0x80 - min(0x7f, (262 - s) * 8)) * 0x01010101u; }
+// the codes with those made 0, but for the bytes of `except`
+__device__ __forceinline__ uint32_t without_nan(uint32_t codes, uint32_t to_top, uint32_t except = 0) {
+    return codes & (except | ~((nan_bytes(codes, to_top) >> 7) * 0xffu));
+}
+// 1.0 (0x38) where there is one and 0 elsewhere
+__device__ __forceinline__ uint32_t where_nan(uint32_t codes, uint32_t to_top) { return (nan_bytes(codes, to_top) >> 7) * 0x38u; }
 // bytes of the four keys from `key` on that lie below `limit`
 __device__ __forceinline__ uint32_t below(int key, int limit) {
     const int n = limit - key;

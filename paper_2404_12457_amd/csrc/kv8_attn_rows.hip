@@ -136,9 +136,10 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_rows_kernel(AttnLaunch a,
         }
         if (key0 + 32 > vis_min) {
             // The frontier.  What a row does not see weighs nothing, whatever the bytes there are: scores are replaced, V behind the
-            // last visible key becomes 0, and a NaN in V that some rows see and others do not goes to the former by a product
-            // of where the NaNs are with who sees them.
+            // last visible key becomes 0, and what bf16 does not hold in a V that some rows see and others do not goes to the former as NaN, by a
+            // product of where such numbers are with who sees them.
             uint32_t nan = 0;
+            const uint32_t to_top[2] = {not_finite_from(sv_now & 255), not_finite_from(sv_now >> 8)};
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int key = key0 + 16 * b + 4 * kg;
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_rows_kernel(AttnLaunch a,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         p.v[b][cc][e] &= keep;
-                        nan |= nan_bytes(p.v[b][cc][e]);
+                        nan |= nan_bytes(p.v[b][cc][e], to_top[b]);
                     }
             }
             if (kv_limit > vis_min && __builtin_amdgcn_ballot_w64(nan != 0) != 0) {
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_rows_kernel(AttnLaunch a,
                 for (int cc = 0; cc < NC; ++cc)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const bf16x8 at = join(widen4(where_nan(p.v[0][cc][e]), 1.f), widen4(where_nan(p.v[1][cc][e]), 1.f));
+                        const bf16x8 at = join(widen4(where_nan(p.v[0][cc][e], to_top[0]), 1.f), widen4(where_nan(p.v[1][cc][e], to_top[1]), 1.f));
 #pragma unroll
                         for (int rt = 0; rt < RT; ++rt) {
                             const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(at, sees[rt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
@@ -174,8 +175,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_rows_kernel(AttnLaunch a,
                             for (int r = 0; r < 4; ++r)
                                 if (n[r] > 0.f) oacc[rt][cc * 4 + e][r] = __builtin_nanf("");
                         }
-                        p.v[0][cc][e] = without_nan(p.v[0][cc][e]);
-                        p.v[1][cc][e] = without_nan(p.v[1][cc][e]);
+                        p.v[0][cc][e] = without_nan(p.v[0][cc][e], to_top[0]);
+                        p.v[1][cc][e] = without_nan(p.v[1][cc][e], to_top[1]);
                     }
             }
         }

@@ -604,3 +604,41 @@ def test_kv8_attention_key_loops_that_end_anywhere_in_a_window(steps, split, d):
         _check(c, d**-0.5)
     finally:
         B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("rows,waves,chunk", [(r, w, c) for r in (16, 32, 128) for w in (4, 8) for c in (0, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_attention_numbers_that_bf16_does_not_hold_count_only_where_they_are_seen(rows, waves, chunk, d):
+    """V of 2^128 and above: the largest bf16 numbers round up to it, and scale bytes above 246 reach further.  A row that sees one
+    has an infinity or NaN in its column; nothing comes to any other row or column."""
+    c = Case([(300, 37), (20, 130), (47, 2)], 8, 2, d, seed=33)
+    c.fill_prefixes()
+    big = float(torch.finfo(torch.bfloat16).max)
+    for at in (3, 20, 36, 37 + 64, 37 + 128):
+        c.v_new[at, 0, 7 * at % d] = big if at % 2 else -big
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    # the last block of the last request, head 1: of its two new tokens the first has one number just below 2^128, the second others above
+    sat, order, tile = 2 * 16 * d, O.byte_of(d, False), c.planes[1][c.h_table[2, 2]]
+    tile[16 * d:2 * 16 * d] = 0
+    tile[sat + 1] = 254                                   # 2^127
+    tile[16 * d + int(order[15, 4])] = 0x3F               # 1.875
+    last = c.planes[1][c.h_table[2, 3]]
+    last[16 * d:2 * 16 * d] = 0
+    last[sat + 1] = 251                                   # 2^124
+    for e, code in ((9, 0x58), (d - 1, 0xFE), (17, 0x57)):  # 16, -448, 15
+        last[16 * d + int(O.byte_of(d, False)[0, e])] = code
+    c.q[-2:, 4:] = 0  # weights of 1 before the division: 1.875 * 2^127 times a larger one would overflow fp32
+    want, tol = _attention(c, c.host(c.q), d**-0.5)
+    planes, inf = c.planes[1].cpu().numpy(), np.zeros_like(want, bool)
+    for r, p, n, at in c.spans():
+        v = O.read_tokens(planes, c.h_table[r], p + n, 2, d, False)
+        for i in range(n):
+            inf[at.start + i] = np.repeat((np.abs(v[:p + i + 1]) >= 2.0**128).any(0), 4, axis=0)
+    assert inf[-1, 4:, [9, d - 1]].all() and not inf[-2, 4:].any() and not inf[-1, 4:, 17].any()
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        got = c.host(_run(c, d**-0.5))
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+    assert np.array_equal(np.isfinite(got), ~inf)
+    assert float((np.abs(got - want) / tol)[~inf].max()) <= 1
