@@ -12,7 +12,7 @@
 // Products.  S^T = K Q^T takes K as it is, in 8 bits, on v_mfma_scale_f32_32x32x64_f8f6f4, which applies the blocks' scales.  A bf16 q
 // has eight significant bits and is the sum of two e4m3 numbers of four: hi = the nearest to q 2^-e, with e from the row's
 // largest |q| as in kv8_append.hip, and lo = the rest times 2^4 (exact as long as they stay normal numbers; below that
-// off by at most 2^-14 of 2^e, 2^-22 of the largest |q|).  Two products at twice the rate of the bf16 ones take as long as one of those, and K needs no
+// off by at most 2^-14 of 2^e, 2^-21.8 of the largest |q|, which is above 224 2^e).  Two products at twice the rate of the bf16 ones take as long as one of those, and K needs no
 // conversion and half the LDS reads.  The matrix unit lines up 16 products at a time with 16 bits below the largest and sums these in
 // fp32: 8e-6 of sum |q k| on unit-variance numbers, 2^-12 of the largest product at worst.
 // O^T += V^T P^T is v_mfma_f32_32x32x16_bf16: each wave turns its block of V into bf16 on the way into LDS (the conversion applies

@@ -642,3 +642,32 @@ def test_kv8_attention_numbers_that_bf16_does_not_hold_count_only_where_they_are
         B.ragc_debug_set_kv8_plan(0)
     assert np.array_equal(np.isfinite(got), ~inf)
     assert float((np.abs(got - want) / tol)[~inf].max()) <= 1
+
+
+@pytest.mark.parametrize("rows,waves,chunk", [(16, 8, 0), (32, 4, 0), (128, 4, 0), (128, 8, 0), (128, 8, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_attention_of_small_numbers_beside_a_large_one(rows, waves, chunk, d):
+    """q is 2^15 where K is 0, and between 1 and 1.6 where K is 0 or 4: what decides is 2^-15 of the row's largest number, of which
+    the second of two e4m3 numbers keeps steps of 2^-7 of 1.  One key in 100 is of the second kind, V 1 there and -1 elsewhere, so that the weights
+    are of one size and the output follows the score by up to half.
+    A score is off by at most off = scale (2^-12 sum |q K| + 2^-21 max|q| sum |K|) = 2^-12 * 6.4 + 2^-21 * 2^15 * 4 = 0.064, a weight by a factor of
+    e^off, and so are their sums: (e^(2 off) - 1) sum p |v|, with 2^-8 of it for the weights' rounding and 2^-8 of the output for its own."""
+    c = Case([(0, 230), (0, 60)], 8, 2, d, seed=35)
+    kind = torch.cat([torch.arange(n, device="cuda") % 100 == 0 for n in (230, 60)])
+    c.k_new.zero_()
+    c.k_new[kind, :, 5] = 4.0
+    c.v_new.copy_(torch.where(kind, 1.0, -1.0)[:, None, None].expand_as(c.v_new))
+    c.q.copy_(torch.from_numpy(c.rng.uniform(1, 1.6, c.q.shape).astype(np.float32)))
+    c.q[:, :, 0] = 2.0**15
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    q = c.host(c.q)
+    want, _ = _attention(c, q, 1.0)
+    off = 2.0**-12 * 4 * np.abs(q[..., 5:6]) + 2.0**-21 * 2.0**15 * 4
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        got = c.host(_run(c, 1.0))
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+    assert (np.abs(got - want) <= 2.0**-8 * np.abs(want) + 2.0**-8 + np.expm1(2 * off)).all()
+    if rows < 128:  # the products of these are exact: fp32 roundings of an exponent of 9.2 (two) and of exp2 in the weights, twice
+        assert (np.abs(got - want) <= 2.0**-8 * np.abs(want) + 2.0**-8 + 4e-6).all()

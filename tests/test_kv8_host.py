@@ -71,6 +71,24 @@ def test_rotation_keeps_lengths_and_relative_angles(interleaved):
     assert np.array_equal(O.rotate(x, 9, cs, interleaved)[..., 32:], x[..., 32:])
 
 
+def test_a_row_of_q_as_two_e4m3_numbers_is_off_by_the_documented_bound():
+    """hi = nearest to q 2^-e, lo = nearest to 16 times the rest.  Elements far below the row's largest lose bits: their own error is
+    not bounded by 2^-12 of them, only by 2^-21 of the largest."""
+    g = np.random.Generator(np.random.PCG64(8))
+    m = (128 + g.integers(0, 128, (500, 64))) / 128 * g.choice([-1, 1], (500, 64))  # the 8 significant bits of a bf16 number
+    q = np.ldexp(m, g.integers(-30, 1, (500, 64)))
+    worst = 0.0
+    for row in q:
+        top = np.abs(row).max()
+        e = O.scale_byte(top) - 127
+        f = np.ldexp(row, -e)
+        hi = O.VALUES[O.encode(f)]
+        off = np.abs(hi + O.VALUES[O.encode((f - hi) * 16)] / 16 - f) * 2.0**e
+        assert (off <= 2.0**-21 * top).all() and (off[np.abs(row) > 2.0**-13 * top] == 0).all()
+        worst = max(worst, float((off / np.abs(row)).max()))
+    assert worst > 2.0**-12
+
+
 # ---- the refusals ---------------------------------------------------------------------------
 def _pool(dtype=B.RAGC_DTYPE_BF16, **kw):
     args = dict(k=A, v=A, num_blocks=64, kv_heads=2, head_dim=128, dtype=dtype)
