@@ -671,3 +671,44 @@ def test_kv8_attention_of_small_numbers_beside_a_large_one(rows, waves, chunk, d
     assert (np.abs(got - want) <= 2.0**-8 * np.abs(want) + 2.0**-8 + np.expm1(2 * off)).all()
     if rows < 128:  # the products of these are exact: fp32 roundings of an exponent of 9.2 (two) and of exp2 in the weights, twice
         assert (np.abs(got - want) <= 2.0**-8 * np.abs(want) + 2.0**-8 + 4e-6).all()
+
+
+@pytest.mark.parametrize("rows,waves", [(r, w) for r in (16, 32, 128) for w in (4, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.filterwarnings("ignore:invalid value")
+def test_kv8_attention_nan_in_k_in_every_layout(rows, waves, d):
+    """A key of one head that is NaN: in the frontier, in an early tile, and a run of 256 of them, so that a copy of 16 blocks and the
+    waves in it see nothing else (a sum that is NaN beside a maximum that was never raised)."""
+    c = Case([(700, 37), (20, 130), (0, 600)], 8, 2, d, seed=36)
+    c.fill_prefixes()
+    for at in (30, 37 + 5, 37 + 100):
+        c.k_new[at, 0, 7 * at % d] = float("nan")
+    c.k_new[167 + 256:167 + 512, 1] = float("nan")
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    want, tol = _attention(c, c.host(c.q), d**-0.5)
+    try:
+        for chunk in (0, 16):
+            B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+            got = c.host(_run(c, d**-0.5))
+            assert np.array_equal(np.isnan(got), np.isnan(want))
+            assert float(np.nanmax(np.abs(got - want) / tol)) <= 1
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("rows,waves,chunk", [(0, 8, 0), (16, 8, 16), (32, 4, 0), (128, 4, 0), (128, 8, 16)])
+def test_kv8_attention_of_requests_that_read_the_same_blocks(rows, waves, chunk):
+    """Five questions about one document, one of them about its first 20 blocks: its blocks are in every table."""
+    lens = [(480, 1), (480, 40), (480, 3), (320, 17), (480, 16)]
+    c = Case(lens, 8, 2, 128, seed=37)
+    for r, (p, _) in enumerate(lens[1:], 1):
+        c.h_table[r, :p // 16] = c.h_table[0, :p // 16]
+    c.dev[3].copy_(torch.from_numpy(c.h_table))
+    c.fill_prefixes()
+    B.ragc_batch_validate(c.pool, c.batch, True)
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        _check(c, 128**-0.5)
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
