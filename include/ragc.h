@@ -197,7 +197,8 @@ int ragc_version(void);
 const char* ragc_last_error(void);
 
 /* Bytes of K/V cache one token occupies in a model: 2 * layers * kv_heads *
- * head_dim * sizeof(dtype) (the KV Size column of the paper's model table).
+ * head_dim * sizeof(dtype) (the KV Size column of the paper's model table); of 8-bit pools
+ * a sixteenth of a block, scales and padding included, for each plane and layer.
  * Returns 0 on bad arguments. */
 int64_t ragc_kv_bytes_per_token(int32_t layers, int32_t kv_heads, int32_t head_dim, int32_t dtype);
 

@@ -43,9 +43,10 @@ int esize_of(int32_t dtype) { return dtype == RAGC_DTYPE_BF16 ? 2 : dtype == RAG
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Bytes of one block of a plane of an 8-bit pool: the tiles, then a scale byte per kv head, to the next multiple of 16.
-int64_t kv8_block_bytes(const ragc_kv_pool* pool) {
-    return (int64_t)pool->kv_heads * RAGC_BLOCK_SIZE * pool->head_dim + ((int64_t)pool->kv_heads + 15) / 16 * 16;
+int64_t kv8_block_bytes(int32_t kv_heads, int32_t head_dim) {
+    return (int64_t)kv_heads * RAGC_BLOCK_SIZE * head_dim + ((int64_t)kv_heads + 15) / 16 * 16;
 }
+int64_t kv8_block_bytes(const ragc_kv_pool* pool) { return kv8_block_bytes(pool->kv_heads, pool->head_dim); }
 
 // eight_bit: 1 = an 8-bit pool is required, 0 = none is accepted, -1 = either
 int check_pool(const ragc_kv_pool* pool, int eight_bit = 0) {
@@ -894,7 +895,8 @@ const char* ragc_last_error(void) { return g_err; }
 
 int64_t ragc_kv_bytes_per_token(int32_t layers, int32_t kv_heads, int32_t head_dim, int32_t dtype) {
     const int es = esize_of(dtype);
-    if (layers <= 0 || kv_heads <= 0 || head_dim <= 0 || es == 0) return 0;
+    if (layers <= 0 || kv_heads <= 0 || head_dim <= 0 || (es == 0 && dtype != RAGC_DTYPE_E4M3)) return 0;
+    if (dtype == RAGC_DTYPE_E4M3) return (int64_t)2 * layers * (kv8_block_bytes(kv_heads, head_dim) / RAGC_BLOCK_SIZE);  // whole multiples of 16
     return (int64_t)2 * layers * kv_heads * head_dim * es;
 }
 

@@ -198,6 +198,12 @@ def test_swap_of_8_bit_pools_counts_the_scales():
     assert B.ragc_kv_swap(_pool8(), A, A, need, 4, np.zeros(0, np.int32), np.zeros(0, np.int32), B.RAGC_SWAP_TO_HOST) == 0
 
 
+def test_bytes_per_token_of_8_bit_pools_count_the_scales():
+    for layers, heads, d in ((32, 8, 128), (1, 1, 64), (80, 17, 128), (7, 32, 64)):
+        assert 16 * B.ragc_kv_bytes_per_token(layers, heads, d, B.RAGC_DTYPE_E4M3) == 2 * layers * B.kv8_block_bytes(heads, d)
+    assert B.ragc_kv_bytes_per_token(0, 8, 128, B.RAGC_DTYPE_E4M3) == 0
+
+
 def _attn_code(pool=None, batch=None, q=A, o=A, hq=8, scale=0.1, flags=0, ws=None, n=0):
     return _code(B.ragc_kv8_attn, pool or _pool8(), batch or _batch(), q, o, hq, scale, flags, ws, n)
 
