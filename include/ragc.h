@@ -308,7 +308,8 @@ int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void
  *   q, q_out    [device] [sum new_len][q_heads][head_dim]; both NULL with q_heads 0 where Q is not to be turned
  *   k_out       [device] the turned K packed like k_new, what ragc_prefill_attn takes for k_new (without
  *               RAGC_ATTN_APPEND_FUSED: the pool has the rows already); NULL where only the pool is wanted
- * q_out may be q and k_out k_new (turned in place); otherwise an output overlaps no input.
+ * q_out may be q and k_out k_new (turned in place); otherwise the rows that the call writes to q_out and k_out overlap none of those
+ * that it reads, nor each other, nor cos_sin: refused.  Nor may the pool's planes overlap any of these, which is not checked.
  * All device arrays are read when the work runs; a captured call replays with the sum of new_len of the capture. */
 int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q,
                         const void* k_new, const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream);

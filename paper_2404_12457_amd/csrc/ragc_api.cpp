@@ -850,6 +850,16 @@ int check_in_place(const void* in, const void* out, int64_t bytes, const char* w
     return RAGC_OK;
 }
 
+// bytes of memory that a call reads or writes
+struct Extent {
+    uintptr_t at, bytes;  // 0 bytes: not given
+    const char* name;
+};
+int check_apart(const Extent& out, const Extent& other) {
+    if (out.bytes && other.bytes && out.at < other.at + other.bytes && other.at < out.at + out.bytes) return fail(RAGC_ERR_SHAPE, "%s overlaps %s", out.name, other.name);
+    return RAGC_OK;
+}
+
 // Both appends with a rotation; an 8-bit pool takes bf16 rows and may come without one.
 int append_rope_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
                      const void* v_new, void* q_out, void* k_out, int32_t q_heads, void* stream) {
@@ -876,6 +886,20 @@ int append_rope_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const ra
     if (int rc = check_in_place(q, q_out, q_heads * head_bytes, "q_out")) return rc;
     if (k_out)
         if (int rc = check_in_place(k_new, k_out, pool->kv_heads * head_bytes, "k_out")) return rc;
+    // workgroups write some rows while others read theirs: the outputs lie apart from all that is not theirs to turn in place
+    const auto rows_of = [&](const void* p, int32_t heads, const char* name) {
+        const uintptr_t row = (uintptr_t)heads * pool->head_dim * es;
+        return Extent{reinterpret_cast<uintptr_t>(p) + h.new_start[0] * row, p ? info.total_new * row : 0, name};
+    };
+    const Extent outs[2] = {rows_of(q_out, q_heads, "q_out"), rows_of(k_out, pool->kv_heads, "k_out")};
+    const Extent angles = {reinterpret_cast<uintptr_t>(rope ? rope->cos_sin : nullptr), rope ? (uintptr_t)rope->positions * rope->rot_dim * sizeof(float) : 0, "rope->cos_sin"};
+    const Extent v_rows = rows_of(v_new, pool->kv_heads, "v_new");
+    if (int rc = check_apart(outs[0], outs[1])) return rc;
+    if (int rc = check_apart(outs[0], rows_of(k_new, pool->kv_heads, "k_new"))) return rc;
+    if (int rc = check_apart(outs[1], rows_of(q, q_heads, "q"))) return rc;
+    for (const Extent& out : outs)
+        for (const Extent& other : {v_rows, angles})
+            if (int rc = check_apart(out, other)) return rc;
     const ragc::RopeArgs args = {rope ? rope->cos_sin : nullptr, rope ? rope->rot_dim : 0, rope ? rope->interleaved : 0};
     const ragc::RopeRows rows = {q, k_new, v_new, q_out, k_out, pool->k, pool->v, q_heads, (int32_t)info.total_new};
     const ragc::PagedBatch pb = make_paged(pool, batch);

@@ -163,6 +163,26 @@ def test_rope_append_refuses_what_is_its_own():
     assert _rope_code(ko=FAR + 8) == B.RAGC_ERR_ALIGN
 
 
+def test_appends_refuse_outputs_that_overlap_what_others_read():
+    """Five rows from number 7 on: q and q_out have 8 heads, the rest 2.  Arrays a megabyte apart, one of them moved."""
+    b, mb, row = _batch(p=(10,), n=(5,), start=(7, 12)), 1 << 20, 128 * 2
+    at = dict(q=A, k=A + mb, v=A + 2 * mb, qo=A + 3 * mb, ko=A + 4 * mb)
+    rows = {n: (at[n] + 7 * h * row, at[n] + 12 * h * row) for n, h in dict(q=8, k=2, v=2, qo=8, ko=2).items()}
+    heads = dict(qo=8, ko=2)
+    for out, other in (("qo", "k"), ("qo", "v"), ("qo", "ko"), ("ko", "q"), ("ko", "v"), ("ko", "qo")):
+        first, end = rows[other]
+        for start in (first - 5 * heads[out] * row + 16, first, end - 16):  # of the rows that the call writes
+            assert _rope_code(batch=b, **{**at, out: start - 7 * heads[out] * row}) == B.RAGC_ERR_SHAPE, (out, other, start)
+            assert "overlaps" in B.ragc_last_error()
+        if other not in ("ko", "qo"):
+            assert "_new" in B.ragc_last_error() or other == "q"
+    for start in (A + 5 * mb, A + 5 * mb + 64 * 128 * 4 - 16):
+        rope = _rope(cos_sin=A + 5 * mb)
+        assert _rope_code(batch=b, rope=rope, **{**at, "ko": start - 7 * 2 * row}) == B.RAGC_ERR_SHAPE and "cos_sin" in B.ragc_last_error()
+        assert _append8_code(batch=b, rope=rope, q=A, k=A + mb, v=A + 2 * mb, qo=start - 7 * 8 * row) == B.RAGC_ERR_SHAPE
+    assert _append8_code(q=A, k=A + mb, v=A + 2 * mb, qo=A + mb) == B.RAGC_ERR_SHAPE and "k_new" in B.ragc_last_error()  # rows from number 0 on
+
+
 def test_kv8_append_refuses_what_is_its_own():
     for dtype in (B.RAGC_DTYPE_F32, B.RAGC_DTYPE_BF16, 3):
         assert _append8_code(pool=_pool(dtype)) == B.RAGC_ERR_SHAPE
