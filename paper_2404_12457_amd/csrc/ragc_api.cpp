@@ -10,6 +10,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <vector>
 
 #include "ragc_internal.h"
@@ -822,13 +823,22 @@ int prefill_attn_impl(const ragc_kv_pool* pool, const ragc_batch* batch, const v
     return run_bf16_plan(a, h, plan, s);
 }
 
-// The host side of a call allocates a little; nothing it throws leaves a C entry point.
+// The host side of a call allocates a little; nothing it throws leaves a C entry point.  Called in a catch (...) block.
+int host_failed() {
+    try {
+        throw;
+    } catch (const std::bad_alloc&) {
+        return fail(RAGC_ERR_HIP, "out of host memory");
+    } catch (...) {
+        return fail(RAGC_ERR_HIP, "an exception on the host");
+    }
+}
 template <class F>
 auto guarded(const F& f) noexcept -> decltype(f()) {
     try {
         return f();
     } catch (...) {
-        return fail(RAGC_ERR_HIP, "out of host memory");
+        return host_failed();
     }
 }
 
@@ -933,7 +943,7 @@ int ragc_debug_set_attn_plan(int32_t variant, int32_t splits) {
     return RAGC_OK;
 }
 
-int ragc_debug_get_attn_plan(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags, int32_t* plan) {
+int ragc_debug_get_attn_plan(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags, int32_t* plan) try {
     g_err[0] = 0;
     if (int rc = check_pool(pool)) return rc;
     if (flags & ~kAttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
@@ -961,6 +971,8 @@ int ragc_debug_get_attn_plan(const ragc_kv_pool* pool, const ragc_batch* batch, 
     plan[1] = p.rows_kernel ? p.waves : p.variant == ragc::kAttnVariantTwoGroups ? 8 : 4;
     plan[2] = p.splits;
     return RAGC_OK;
+} catch (...) {
+    return host_failed();
 }
 
 int ragc_debug_set_attn_product(int32_t rows) {
@@ -970,7 +982,7 @@ int ragc_debug_set_attn_product(int32_t rows) {
     return RAGC_OK;
 }
 
-int ragc_debug_get_attn_product(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) {
+int ragc_debug_get_attn_product(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) try {
     int32_t plan[3];
     if (int rc = ragc_debug_get_attn_plan(pool, batch, q_heads, flags, plan)) return rc;
     if (pool->dtype != RAGC_DTYPE_BF16 || pool->head_dim != 128 || plan[0] != ragc::kAttnRowsPerItem || plan[2] != 1) return 0;
@@ -980,9 +992,11 @@ int ragc_debug_get_attn_product(const ragc_kv_pool* pool, const ragc_batch* batc
     Bf16Plan p;
     if (int rc = plan_bf16(pool, batch, h, q_heads / pool->kv_heads, flags, &p)) return rc;
     return p.quarters ? 16 : 32;
+} catch (...) {
+    return host_failed();
 }
 
-int ragc_batch_validate(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t writes_new_tokens) {
+int ragc_batch_validate(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t writes_new_tokens) try {
     g_err[0] = 0;
     if (int rc = check_pool(pool, -1)) return rc;
     BatchInfo info;
@@ -990,9 +1004,11 @@ int ragc_batch_validate(const ragc_kv_pool* pool, const ragc_batch* batch, int32
     if (int rc = check_batch(pool, batch, true, true, &h, &info)) return rc;
     if (batch->num_reqs == 0) return RAGC_OK;
     return validate_batch(pool, batch, h, writes_new_tokens != 0);
+} catch (...) {
+    return host_failed();
 }
 
-int64_t ragc_prefill_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) {
+int64_t ragc_prefill_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) try {
     g_err[0] = 0;
     if (int rc = check_pool(pool)) return rc;
     if (flags & ~kAttnFlags) return fail(RAGC_ERR_SHAPE, "unknown flags 0x%x", flags);
@@ -1005,19 +1021,25 @@ int64_t ragc_prefill_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* 
     Bf16Plan plan;
     if (int rc = plan_bf16(pool, batch, h, q_heads / pool->kv_heads, flags, &plan)) return rc;
     return plan.workspace;
+} catch (...) {
+    return host_failed();
 }
 
 int ragc_prefill_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, const void* k_new,
                       const void* v_new, void* out, int32_t q_heads, float softmax_scale, uint32_t flags,
-                      void* workspace, size_t workspace_bytes, void* stream) {
+                      void* workspace, size_t workspace_bytes, void* stream) try {
     return prefill_attn_impl(pool, batch, q, k_new, v_new, out, q_heads, softmax_scale, flags, workspace, workspace_bytes,
                              false, stream);
+} catch (...) {
+    return host_failed();
 }
 
 int ragc_prefill_attn_static(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, const void* k_new,
                              const void* v_new, void* out, int32_t q_heads, float softmax_scale, uint32_t flags,
-                             void* stream) {
+                             void* stream) try {
     return prefill_attn_impl(pool, batch, q, k_new, v_new, out, q_heads, softmax_scale, flags, nullptr, 0, true, stream);
+} catch (...) {
+    return host_failed();
 }
 
 int64_t ragc_kv8_attn_workspace(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t q_heads, uint32_t flags) {
@@ -1101,7 +1123,7 @@ int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void*
     });
 }
 
-int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new, void* stream) {
+int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void* k_new, const void* v_new, void* stream) try {
     g_err[0] = 0;
     if (int rc = check_pool(pool)) return rc;
     BatchInfo info;
@@ -1115,6 +1137,8 @@ int ragc_kv_append(const ragc_kv_pool* pool, const ragc_batch* batch, const void
                                              esize_of(pool->dtype), static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "append launch");
     return RAGC_OK;
+} catch (...) {
+    return host_failed();
 }
 
 int ragc_kv_append_rope(const ragc_kv_pool* pool, const ragc_batch* batch, const ragc_rope* rope, const void* q, const void* k_new,
@@ -1163,7 +1187,7 @@ int ragc_kv_gather(const ragc_kv_pool* pool, const ragc_batch* batch, int32_t re
 
 int ragc_kv_swap(const ragc_kv_pool* pool, void* host_k, void* host_v, int64_t host_block_stride_elems,
                  int32_t num_host_slots, const int32_t* dev_block_ids, const int32_t* host_slots, int32_t n,
-                 int32_t direction, uint32_t flags, void* stream) {
+                 int32_t direction, uint32_t flags, void* stream) try {
     g_err[0] = 0;
     if (int rc = check_pool(pool, -1)) return rc;
     if (!host_k || !host_v) return fail(RAGC_ERR_NULL, "host_k / host_v is NULL");
@@ -1237,6 +1261,8 @@ int ragc_kv_swap(const ragc_kv_pool* pool, void* host_k, void* host_v, int64_t h
         if (e != hipSuccess) return hip_fail(e, "swap kernel launch");
     }
     return RAGC_OK;
+} catch (...) {
+    return host_failed();
 }
 
 }  // extern "C"

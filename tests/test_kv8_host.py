@@ -1,6 +1,9 @@
 """Rotation and 8-bit cache without a GPU: the oracle against hand-worked and brute-force values, and the refusals of the
 entry points, which come before anything touches the device."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -338,6 +341,26 @@ def test_rows_that_whole_numbers_do_not_hold_are_refused():
     assert _code(B.ragc_kv8_attn_workspace, _pool8(num_blocks=1 << 21), big, 8) == B.RAGC_ERR_RANGE
     wide = _batch(p=(0,), n=(2000,), stride=200)
     assert _attn_code(pool=_pool8(kv_heads=1), batch=wide, hq=2048) == B.RAGC_ERR_RANGE
+
+
+@pytest.mark.parametrize("call", ["ragc_batch_validate(pool, batch, 1)", "ragc_kv8_attn(pool, batch, A, A, 8, 0.1, B.RAGC_ATTN_VALIDATE)",
+                                  "ragc_prefill_attn(pool16, batch, A, A, A, A, 8, 0.1, B.RAGC_ATTN_VALIDATE)"])
+def test_host_memory_that_is_not_there_is_an_error(call):
+    """A block table of 2^49 bytes to be read back.  In a process of its own, which an exception through the C entry would end."""
+    code = f"""
+import numpy as np
+from paper_2404_12457_amd import binding as B
+A, n = {A}, 65535
+pool, pool16 = (B.make_pool(A, A, 64, 2, 128, t) for t in (B.RAGC_DTYPE_E4M3, B.RAGC_DTYPE_BF16))
+lens = [np.ones(n, np.int32), np.ones(n, np.int32), np.arange(n + 1, dtype=np.int32)]
+batch = B.make_batch(n, 2**31 - 1, A, A, A, A, *lens, None)
+try:
+    B.{call}
+except B.RagcError as e:
+    print(e.code, B.ragc_last_error())
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert got.returncode == 0 and got.stdout == f"{B.RAGC_ERR_HIP} out of host memory\n", got
 
 
 def test_an_output_may_stand_right_behind_its_input():
