@@ -345,13 +345,15 @@ int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, i
  * with every K_j, V_j, those of the new tokens too, from the pool: ragc_kv8_append comes first, on the same stream.
  * Arguments, workspace, lengths under capture and requests without new tokens as for ragc_prefill_attn; q and out are
  * bf16, flags RAGC_ATTN_NO_SPLIT and RAGC_ATTN_VALIDATE.  Softmax and sums are fp32, probabilities are rounded to bf16
- * before the product with V and the output to nearest even.  Where any request of the batch has more than 16 rows (new tokens
- * times q heads per kv head) the library may multiply K in 8 bits in all rows of the call, with q as the sum of two e4m3 numbers,
- * which leaves a score off by scale * (2^-12 sum |q K_j| + 2^-21 max(|q|, 2^-115) sum |K_j|) at most, the maximum over the
- * row's elements (8e-6 on unit-variance numbers; elements of q below 2^-13 of that maximum lose bits).  A key or value that a row does not see counts nothing there, whatever its
- * bytes; NaN in one that it sees reaches it.  A value of 2^128 or more, which ragc_kv8_append makes of bf16 numbers from 1.9375 * 2^127 on, is
- * an infinity, and the column of a row that sees it an infinity or NaN; weights of up to 2^8 come before the division, so sums may overflow
- * from 2^120 / keys on. */
+ * before the product with V and the output to nearest even.
+ *   Scores: where any request of the batch has more than 16 rows (new tokens times q heads per kv head) the library may
+ * multiply K in 8 bits in all rows of the call, with q as the sum of two e4m3 numbers.  A score is then off by at most
+ * scale * (2^-12 sum |q K_j| + 2^-21 max(|q|, 2^-115) sum |K_j|), the maximum over the row's elements (8e-6 on
+ * unit-variance numbers; elements of q below 2^-13 of that maximum lose bits).
+ *   What is not finite: a key or value that a row does not see counts nothing there, whatever its bytes; NaN in one that it
+ * sees reaches it.  A value of 2^128 or more, which ragc_kv8_append makes of bf16 numbers from 1.9375 * 2^127 on, is an
+ * infinity, and the column of a row that sees it an infinity or NaN; weights of up to 2^8 come before the division, so
+ * sums may overflow from 2^120 / keys on. */
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -20,10 +20,11 @@
 // from any offset, (n + 30) / 16, so no list has to be made on the host and a captured launch follows the device arrays.
 // Workgroups behind the last item of the blocks turn Q (kv_rope.h).
 //
-// What bounds it: HBM on large calls, the chain of memory trips and the fetching of instructions on small ones.  16 requests of 6.6k
-// tokens in all, 32/8 heads of 128: 38 us (4.6 TB/s), of these 22 for Q, 4 for the fp64 rotation of K; angles are fetched in fours and both ends
-// of a pair stay in one lane (62 us with an exchange between lanes).  64 tokens 7.2 us, one token 7.7 (12 with one kernel for every kind of
-// rotation).
+// What bounds it: HBM on large calls, the chain of memory trips, of rotations and of the fetching of instructions on small ones: a lane turns,
+// rounds and converts 32 numbers one after the other, for one token too, whose row all sixteen lanes of a group repeat.  16 requests
+// of 7.6k tokens in all, 32/8 heads of 128: 38 us (4.6 TB/s), of these 22 for Q, 4 for the fp64 rotation of K; angles are fetched in fours and both
+// ends of a pair stay in one lane (62 us with an exchange between lanes).  Pairs of neighbours 44 us, head_dim 64 25, K as it is and no Q 12
+// (3.9 TB/s).  64 tokens of 64 requests 7.1 us (neighbours 7.4, K as it is 5.7), one token 7.6 (12 with one kernel for every kind of rotation).
 #include <type_traits>
 
 #include "kv8_codes.h"

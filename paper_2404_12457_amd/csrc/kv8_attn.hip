@@ -22,8 +22,8 @@
 // row's reference exponent is raised only when a tile's probabilities against it sum to more than 2^8.
 //
 // What bounds it: matrix and vector units, of which the waves of a SIMD use one after the other more than side by side: of a CU's busy time
-// the products take 0.52, vector instructions 0.47 (16 ragged requests, 32/8 heads of 128: 233 us, 1036 TFLOP/s of the 1236 that a large bf16
-// product reaches; the bf16 cache's kernel takes 289 for such a batch).  4 x (4096+128), 64/8 heads: 67 us, 1030 TFLOP/s.  A step of
+// the products take 0.52, vector instructions 0.47 (16 ragged requests, 32/8 heads of 128: 233 us, 1034 TFLOP/s of the 1236-1290 that a large bf16
+// product reaches; the bf16 cache's kernel takes 289 for such a batch).  4 x (4096+128), 64/8 heads: 66.7 us, 1047 TFLOP/s.  A step of
 // eight waves takes 4215 cycles at head_dim 128: 1090 for the scores, 1300 for softmax and V's conversion, 550 for P V as a wave sees them, and 1160 until its
 // sister on the SIMD is done; the products of both need 2048.  At head_dim 64 the vector part is twice the products.
 // What is brought for later steps is issued under the products: without a branch 71 instead of 77 us (4 x (4096+128)), and

@@ -13,9 +13,11 @@
 // and four keys of each block, which is also how it holds V.  The probabilities are rounded to bf16 for the product, like those of
 // the bf16 kernels, and the row sum is taken over the rounded ones.
 //
-// Measured at 64/8 heads of 128: 64 requests of 512-2048 keys, a token each, 30.6 us (5.4 TB/s); 128 of 200-1000, 32/8 heads, 35 us with 8 waves,
-// 30.4 with 4, two workgroups to a CU.  Two row tiles (32 rows): 512 items of 2064 keys 27.3 us with
-// 4 waves, 30.8 with 8; 256 of 4256 keys 31 and 26.
+// Measured over three states in rotation (none stays in a cache): 64 requests of 512-2048 keys, a token each, 64/8 heads of 128, 35.0 us with 4
+// waves, two workgroups to a CU, 34.1 with 8 (4.7 and 4.8 TB/s: the longest requests run on when the rest is done; 63 of 2000 keys, 32/8
+// heads, 5.2 TB/s); 128 of 200-1000, 32/8 heads, 32.8 and 37.4; the first of head_dim 64 19.0 (4.3 TB/s, the same tail).  Two row tiles (32
+// rows), four tokens of each of those requests: 37.9 and 38.3; 512 items of 2064 keys that two share 36.7 and 41.1, 256 of 4320 that four share 34.8
+// and 28.1.
 // Windows of ids through LDS, or two pairs of blocks under way, changed nothing.
 #include "kv8_attn_common.h"
 

@@ -4,7 +4,7 @@
 //
 // What bounds it: HBM on large calls (every row read once and written once), the trips to memory in a row on small ones (lengths, then
 // the table and the angles' rows, with the sources under way).  Four heads per workgroup and row keep 128 bytes per thread in flight and
-// share the angles.  16 requests of 6.6k tokens in all, 32/8 heads of 128 in bf16, Q turned too, 185 MB moved: 39.3 us, 4.7 TB/s
+// share the angles.  16 requests of 7.4k tokens in all, 32/8 heads of 128 in bf16, Q turned too, 185 MB moved: 39.2 us, 4.7 TB/s
 // (a large copy runs at 5.05 on the same card); a step of 64 requests, 64/8 heads, 5.3 us.
 #include "kv_rope.h"
 

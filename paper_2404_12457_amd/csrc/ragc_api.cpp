@@ -519,15 +519,18 @@ inline int64_t kv8_copies(const HostMeta& h, int r, int chunk) {
 // The plan is the cheapest of what can run the batch, by a cost model in microseconds with measured constants.  A call takes `start` (launch,
 // prologue, epilogue, and what the first tiles wait for).  A workgroup takes `alone` per 16-key block while it has a CU for itself, `shared`
 // where every CU is busy, and then `each` for its own beginning and end: one that has the CU for itself hides nothing of that.
-// Measured, at head_dim 128 where not said otherwise:
-//   16 rows, memory-bound: 64 x (512-2048) keys, 64/8 heads, 8 waves 30.6 us (5.4 TB/s); 128 x (200-1000), 32/8 35 us with 8 waves, 30.4 with
-//     4, of which two workgroups share a CU; one step of 10000 keys, not split, 38.5 with 8, 55 with 4
-//   32 rows: 512 items of 2064 keys 27.3 us with 4 waves, 30.8 with 8; 256 of 4256 keys 31 and 26
-//   128 rows: 256 items of 4224 keys 67 us with 8 waves, 76 with 4 (32 rows: 1024 items, 118); 754 of 400-800 keys 56 and 42
-//   128 rows of 64: 1024 items of 2128 keys 84 us with 8 waves, two workgroups to a CU, 82 with 4; 384 of 2175 40.6 and 44.9
+// Measured per call among others, three states in rotation, at head_dim 128 where not said otherwise:
+//   16 rows, memory-bound: 64 x (512-2048) keys, 64/8 heads, 34.5 us with 8 waves, 35.6 with 4, of which two workgroups share a CU (the plan takes
+//     4); 128 x (200-1000), 32/8, 37.9 and 33.3 (4); 47 x 225, 64/8, 10.7 and 8.2 (8: of 120 random batches the one that it
+//     fits worst); one step of 10000 keys, not split, 38.7 and 53.9
+//   32 rows: 512 items of 2064 keys 41.1 us with 8 waves, 36.7 with 4; 256 of 4320 28.1 and 34.8; 512 of 512-2048 that share no key 38.7
+//     and 38.4, which is memory's time and not in the constants
+//   128 rows: 256 items of 4224 keys 67.5 us with 8 waves, 74.3 with 4 (32 rows: 1024 items, 85.9); 768 of 400-800 keys 50.6 and 38.8
+//   128 rows of 64: 1024 items of 2128 keys 85.3 us with 8 waves, two workgroups to a CU, 84.8 with 4; 384 of 2175 41.2 and 44.0; 376 of
+//     350-2300 29.9 and 30.5, but 32 rows with 4 waves 28.6 (the plan takes 128 and 8)
 // Long ranges are also tried in copies of equal length, one per slot, for which a merge has to be paid: a launch and the partial
-// results' way to memory and back (one step of 100003 keys 500 -> 43 us; 4 of 4096, 64/8 heads, 18.6 -> 14; a prompt of 8000+300, 32/8 heads,
-// in items of 128 rows 112 -> 56, of 64 numbers a head 76 -> 40).
+// results' way to memory and back (one step of 100003 keys 502 -> 45 us; 4 of 4096, 64/8 heads, 18.8 -> 14.4; a prompt of 8000+300, 32/8 heads,
+// in items of 128 rows 106 -> 51, of 64 numbers a head 74 -> 35).
 struct Kv8Kind {
     int rows, waves, per_cu;
     double start, alone, shared, each;
