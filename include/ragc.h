@@ -351,9 +351,9 @@ int ragc_debug_get_kv8_plan(const ragc_kv_pool* pool, const ragc_batch* batch, i
  * scale * (2^-12 sum |q K_j| + 2^-21 max(|q|, 2^-115) sum |K_j|), the maximum over the row's elements (8e-6 on
  * unit-variance numbers; elements of q below 2^-13 of that maximum lose bits).
  *   What is not finite: a key or value that a row does not see counts nothing there, whatever its bytes; NaN in one that it
- * sees reaches it.  A value of 2^128 or more, which ragc_kv8_append makes of bf16 numbers from 1.9375 * 2^127 on, is an
- * infinity, and the column of a row that sees it an infinity or NaN; weights of up to 2^8 come before the division, so
- * sums may overflow from 2^120 / keys on. */
+ * sees reaches it.  A number of 2^128 or more, which ragc_kv8_append makes of bf16 numbers from 1.9375 * 2^127 on, is an
+ * infinity: in a value that a row sees its column of the output is an infinity or NaN, in a key the row's score may be.
+ * Weights of up to 2^8 come before the division, so sums may overflow for values from 2^120 / keys on. */
 int ragc_kv8_attn(const ragc_kv_pool* pool, const ragc_batch* batch, const void* q, void* out, int32_t q_heads, float softmax_scale,
                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 

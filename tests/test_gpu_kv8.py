@@ -712,3 +712,25 @@ def test_kv8_attention_of_requests_that_read_the_same_blocks(rows, waves, chunk)
         _check(c, 128**-0.5)
     finally:
         B.ragc_debug_set_kv8_plan(0)
+
+
+@pytest.mark.parametrize("rows,waves,chunk", [(r, w, c) for r in (16, 32, 128) for w in (4, 8) for c in (0, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_attention_keys_that_bf16_does_not_hold_count_only_where_they_are_seen(rows, waves, chunk, d):
+    """K of 2^128 in one head: rows that come before it, and the other head, are as if it were not there."""
+    c = Case([(300, 37), (20, 130)], 8, 2, d, seed=38)
+    c.fill_prefixes()
+    first = {0: 20, 1: 37 + 64}
+    for at in (*first.values(), 30, 37 + 128):
+        c.k_new[at, 0, 7 * at % d] = float(torch.finfo(torch.bfloat16).max)
+    B.ragc_kv8_append(c.pool, c.batch, None, None, c.k_new, c.v_new, None, 0, _stream())
+    free = np.ones((c.rows, c.hq), bool)
+    for r, _, n, at in c.spans():
+        free[first[r]:at.stop, :4] = False
+    want, tol = _attention(c, c.host(c.q), d**-0.5)
+    try:
+        B.ragc_debug_set_kv8_plan(rows, waves, chunk)
+        got = c.host(_run(c, d**-0.5))
+    finally:
+        B.ragc_debug_set_kv8_plan(0)
+    assert float((np.abs(got - want) / tol)[free].max()) <= 1
